@@ -295,6 +295,116 @@ int ssconv_forward_norm(const void* feats, ssconv_dtype dtype, int cin, ssconv_r
                         const ssconv_fields* fields_out /*host*/, double eps, void* y, void* z,
                         hipStream_t stream);
 
+/* ---- norm of a site ----------------------------------------------------------
+ * The normalisation of a residual network's blocks, with no statistics over rows
+ * (so a site's result does not depend on the others, and one site can be served
+ * alone).  Per row and per entry of `fields`, m fields of order l:
+ *   mu = mean of the entry's fields (l = 0; else 0),  v = sum |f - mu|^2 / m,
+ *   y = gain[field] * (f - mu) / sqrt(v + eps)
+ * |f|^2 is the sum over a field's 2l+1 components, a rotation invariant, so the
+ * norm commutes with the steerable representation.  An entry of one scalar
+ * becomes 0.  gain: fp32 [fields], NULL = ones.  Sums, statistics and products are
+ * fp32, one rounding to `dtype`; squares are summed in fp32, so values past
+ * about 1e18 leave its range.  An infinity or NaN stays within its entry of its row
+ * (a NaN makes all of it NaN).
+ *
+ * Rows that a call reads may be a checkpoint of themselves (ssconv_pack): data
+ * then points at the int8 values and exps at their exponent bytes; exps NULL:
+ * rows in `dtype`.
+ *
+ * Forward: x, y [n, C], C = 1..1024.  q, exps (both or neither): also leaves a
+ * checkpoint of x there (x then is in `dtype`).  y may be x's buffer where x is
+ * not a checkpoint.
+ * Backward: dx = the gradient with respect to x of <y, dy>, plus dres (NULL: 0),
+ * the gradient that reaches x past the norm; dgain fp32 [fields] (NULL: skipped)
+ * = sum over rows of dy * y / gain, in a fixed order (deterministic).  dx may be
+ * dy's or dres's buffer.  workspace: device scratch of at least
+ * ssconv_site_norm_workspace_size bytes, 256-byte aligned, needed where dgain is
+ * given; calls that overlap in time need their own.
+ * n = 0: dgain becomes 0, nothing else is written.  Nothing is allocated and the
+ * stream is not synchronised.  Feature buffers need the alignment of their
+ * elements only; no buffers may overlap but those named here.
+ * Errors: E_DTYPE, E_INVALID, E_HIP. */
+typedef struct {
+  const void* data;
+  const uint8_t* exps;
+} ssconv_rows;
+
+int ssconv_site_norm_forward(const ssconv_fields* fields /*host*/, const ssconv_rows* x /*host*/, ssconv_dtype dtype,
+                             int64_t n, double eps, const float* gain, void* y, int8_t* q, uint8_t* exps,
+                             hipStream_t stream);
+size_t ssconv_site_norm_workspace_size(const ssconv_fields* fields /*host*/, int64_t n);
+int ssconv_site_norm_backward(const ssconv_fields* fields /*host*/, const ssconv_rows* x /*host*/, const void* dy,
+                              const void* dres, ssconv_dtype dtype, int64_t n, double eps, const float* gain, void* dx,
+                              float* dgain, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ---- tail of a residual block --------------------------------------------------
+ * What follows a block's convolution, in one pass over the rows: the norm of a
+ * site (above), the gate (Eq. 12), the residual scale and sum, and the norm in
+ * front of the next block.  `fields` are the regular fields (C channels, F
+ * fields, G of them of order > 0); y [n, C + G] is the convolution's output with
+ * the gate channels behind the fields, which the norm takes as one more entry of
+ * G scalars (so fields has at most SSCONV_MAX_ENTRIES - 1 entries where G > 0,
+ * and C + G <= 1024); h [n, C] is the residual stream.
+ *   u = site norm of y with gain_post [F + G]
+ *   g = relu(u) for l = 0 (NaN stays NaN), sigmoid(u_gate) * u for l > 0
+ *   h_out = h + scale[field] * g            (rounded to dtype)
+ *   x_out = site norm of h_out with gain_next [F]
+ * scale, gain_post, gain_next: fp32, NULL = ones.  x_out NULL: no next norm
+ * (gain_next is then NULL too).  y_q, y_exps and h_q, h_exps (each pair both or
+ * neither): checkpoints (ssconv_pack) of y (with the gates as the last entry) and
+ * of h_out.  h_out may be h's buffer.
+ *
+ * Backward: from y and h_out (as rows or as checkpoints), dh [n, C] = gradient of
+ * h_out and dx [n, C] = gradient of x_out (NULL where there was none; h_out may then
+ * be NULL): dy [n, C + G], dh_in [n, C] = gradient of h, and dgain_post, dscale,
+ * dgain_next (fp32, each NULL to skip; dgain_next NULL without dx), summed over the
+ * rows in a fixed order.  relu'(0) = 0.  dh_in may be dh's or dx's buffer.
+ * workspace: as for the norm, ssconv_residual_workspace_size bytes, needed where
+ * one of the three is given.  n = 0, alignment, overlap and errors as for the norm. */
+int ssconv_residual_forward(const ssconv_fields* fields /*host*/, const void* y, const void* h, ssconv_dtype dtype,
+                            int64_t n, double eps, const float* gain_post, const float* scale, const float* gain_next,
+                            void* h_out, void* x_out, int8_t* y_q, uint8_t* y_exps, int8_t* h_q, uint8_t* h_exps,
+                            hipStream_t stream);
+size_t ssconv_residual_workspace_size(const ssconv_fields* fields /*host*/, int64_t n);
+int ssconv_residual_backward(const ssconv_fields* fields /*host*/, const ssconv_rows* y /*host*/,
+                             const ssconv_rows* h_out /*host*/, const void* dh, const void* dx, ssconv_dtype dtype,
+                             int64_t n, double eps, const float* gain_post, const float* scale, const float* gain_next,
+                             void* dy, void* dh_in, float* dgain_post, float* dscale, float* dgain_next,
+                             void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ---- activation checkpoints in 8 bits --------------------------------------------
+ * What a training step keeps of an activation x [n, C] for its backward pass: int8
+ * q [n, C] and one exponent byte per row and block of 32 consecutive channels; the
+ * blocks start anew with every entry of `fields` (so no block mixes orders) and an
+ * entry's last one may be shorter: exps [n, ssconv_packed_blocks(fields)].
+ * With amax = a 2^E the block's largest magnitude, 1 <= a < 2:
+ *   k = max(-126, E - 6 + (a > 127/64)),  q = round to nearest even of x 2^-k,
+ *   byte = k + 127, and q 2^k is the value that is read back (exact in bf16 too).
+ * |x - q 2^k| <= 2^(k-1) <= amax / 127 (and 2^-127 where k = -126).  A block with an infinity
+ * or a NaN has the byte 255 and reads back as NaN.  A checkpoint of 208 channels
+ * in bf16 takes 52% of its memory, in fp32 26%.
+ * C = 1..1024.  n = 0 is a no-op.  Buffers need the alignment of their elements. */
+int64_t ssconv_packed_blocks(const ssconv_fields* fields /*host*/); /* 0 for a bad list */
+int ssconv_pack(const ssconv_fields* fields /*host*/, const void* x, ssconv_dtype dtype, int64_t n, int8_t* q,
+                uint8_t* exps, hipStream_t stream);
+int ssconv_unpack(const ssconv_fields* fields /*host*/, const int8_t* q, const uint8_t* exps, int64_t n,
+                  ssconv_dtype dtype, void* x, hipStream_t stream);
+
+/* ssconv_backward of a convolution whose input is kept as a checkpoint (q, exps over
+ * fields_in, cin = its channels): feats = the values read back (norm = 0), or their
+ * site norm with `eps` and `gain` (norm = 1: the checkpoint is of the residual
+ * stream, and the normed input of the convolution is not kept at all), in `dtype`.
+ * grad_feats is the gradient of that input, before any norm.  The rows are expanded into
+ * the workspace (ssconv_backward_packed_workspace_size bytes, 256-byte aligned) where
+ * grad_coeffs is asked for.  Everything else, errors too, as ssconv_backward. */
+size_t ssconv_backward_packed_workspace_size(ssconv_rulebook_t rb, ssconv_dtype dtype, int cin, int cout);
+int ssconv_backward_packed(const ssconv_fields* fields_in /*host*/, const int8_t* q, const uint8_t* exps, int norm,
+                           double eps, const float* gain, const void* grad_out, ssconv_dtype dtype, int cout,
+                           ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc /*host*/,
+                           const float* basis, void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes,
+                           hipStream_t stream);
+
 /* ---- sparse average pooling (Sec. 3.1, footnote: downsampling is a stride-1
  * convolution followed by average pooling) -----------------------------------
  * rb must be built with ksize = 2, stride = 2, submanifold = 0: its offsets

@@ -18,6 +18,8 @@ Modules
               site centres, re-voxelisation with averaging of merged sites (Sec. 4.1)
     interp    Tensor-to-Point: trilinear interpolation of the zero-filled site grid at
               points, and its adjoint (Sec. 4.1)
+    site      norm of a site (no statistics over rows), tail of a residual block (norm, gate,
+              scale, sum), 8-bit checkpoints with a shared exponent; forward and backward
 
 Readings of the paper that it takes (all pinned by invariants in tests/):
     real SH without Condon-Shortley phase, components ordered m = -l..l;

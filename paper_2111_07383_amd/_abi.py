@@ -22,6 +22,10 @@ class Fields(ctypes.Structure):
     _fields_ = [("n", c_int), ("l", c_int * MAX_ENTRIES), ("mult", c_int * MAX_ENTRIES)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("exps", c_void_p)]
+
+
 class BasisDesc(ctypes.Structure):
     _fields_ = [("in_", Fields), ("out", Fields), ("ksize", c_int), ("n_shells", c_int),
                 ("shells", c_double * MAX_SHELLS), ("eps", c_double), ("jmax", c_int)]
@@ -71,6 +75,25 @@ SIGNATURES = {
                                    c_void_p, c_void_p]),
     "ssconv_interpolate_backward": (c_int, [c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int64, POINTER(c_float),
                                             c_float, c_void_p, c_void_p]),
+    "ssconv_site_norm_forward": (c_int, [POINTER(Fields), POINTER(Rows), c_int, c_int64, c_double, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_void_p]),
+    "ssconv_site_norm_workspace_size": (c_size_t, [POINTER(Fields), c_int64]),
+    "ssconv_site_norm_backward": (c_int, [POINTER(Fields), POINTER(Rows), c_void_p, c_void_p, c_int, c_int64, c_double,
+                                          c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ssconv_residual_forward": (c_int, [POINTER(Fields), c_void_p, c_void_p, c_int, c_int64, c_double, c_void_p,
+                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_void_p]),
+    "ssconv_residual_workspace_size": (c_size_t, [POINTER(Fields), c_int64]),
+    "ssconv_residual_backward": (c_int, [POINTER(Fields), POINTER(Rows), POINTER(Rows), c_void_p, c_void_p, c_int,
+                                         c_int64, c_double, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ssconv_packed_blocks": (c_int64, [POINTER(Fields)]),
+    "ssconv_pack": (c_int, [POINTER(Fields), c_void_p, c_int, c_int64, c_void_p, c_void_p, c_void_p]),
+    "ssconv_unpack": (c_int, [POINTER(Fields), c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p]),
+    "ssconv_backward_packed_workspace_size": (c_size_t, [c_void_p, c_int, c_int, c_int]),
+    "ssconv_backward_packed": (c_int, [POINTER(Fields), c_void_p, c_void_p, c_int, c_double, c_void_p, c_void_p, c_int,
+                                       c_int, c_void_p, c_void_p, POINTER(BasisDesc), c_void_p, c_void_p, c_void_p,
+                                       c_void_p, c_size_t, c_void_p]),
     "ssconv_debug_set": (c_int, [c_int, c_int64]),
     "ssconv_debug_kernel_ms": (c_int, [POINTER(c_int64), POINTER(c_float)]),
 }

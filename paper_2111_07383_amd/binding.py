@@ -6,13 +6,15 @@ etc.).  Tensors must live on the current HIP device; bf16 tensors map to
 SSCONV_BF16 and fp32 tensors to SSCONV_F32.
 """
 import ctypes
+from contextlib import nullcontext
 from ctypes import byref, c_float, c_int, c_int64, c_void_p
-from typing import Optional, Sequence, Tuple
+from dataclasses import dataclass
+from typing import Optional, Sequence, Tuple, Union
 
 import numpy as np
 import torch
 
-from ._abi import BF16, F32, BasisDesc, Fields, check, lib
+from ._abi import BF16, F32, MAX_ENTRIES, BasisDesc, Fields, Rows, check, lib
 
 FieldList = Sequence[Tuple[int, int]]
 
@@ -341,6 +343,320 @@ def norm_backward(fields: FieldList, x: torch.Tensor, dy: torch.Tensor, eps: flo
     check(lib().ssconv_norm_backward(byref(f), _ptr(x), _ptr(dy), _dtype(x), x.shape[0], float(eps), _ptr(dx),
                                      _stream(stream)), "ssconv_norm_backward")
     return dx
+
+
+def _here(*tensors):
+    """The calls below launch on the current device: their tensors have to be there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _on(stream):
+    """Results and scratch of a call on a given stream come from that stream's memory: a block of another stream may
+    still be in use there, or be handed out again there before the call has run."""
+    return nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _field_list(fields: FieldList) -> Tuple[Tuple[int, int], ...]:
+    fields = tuple((int(l), int(m)) for l, m in fields)
+    if not 1 <= len(fields) <= MAX_ENTRIES:
+        raise ValueError(f"a field list has 1 to {MAX_ENTRIES} entries")
+    return fields
+
+
+def gate_fields(fields: FieldList) -> Tuple[Tuple[int, int], ...]:
+    """The fields with their gate channels (one scalar per field of order > 0) as one more entry."""
+    fields = _field_list(fields)
+    g = sum(m for l, m in fields if l > 0)
+    return fields + (((0, g),) if g else ())
+
+
+def packed_blocks(fields: FieldList) -> int:
+    """Exponent bytes of a row of a checkpoint (ssconv_packed_blocks); raises for a bad list."""
+    f = make_fields(_field_list(fields))
+    b = int(lib().ssconv_packed_blocks(byref(f)))
+    if b == 0:
+        raise ValueError(f"bad field list {tuple(fields)}: " + lib().ssconv_last_error().decode())
+    return b
+
+
+@dataclass
+class Packed:
+    """An 8-bit checkpoint of rows [n, C] (ssconv_pack): int8 values [n, C] and one exponent byte per row and block of
+    32 channels of an entry of ``fields``, [n, packed_blocks(fields)]."""
+    fields: Tuple[Tuple[int, int], ...]
+    q: torch.Tensor
+    exps: torch.Tensor
+
+    @property
+    def shape(self):
+        return self.q.shape
+
+    @property
+    def device(self):
+        return self.q.device
+
+    @property
+    def nbytes(self) -> int:
+        return self.q.numel() + self.exps.numel()
+
+    @staticmethod
+    def empty(fields: FieldList, n: int, device) -> "Packed":
+        fields = _field_list(fields)
+        return Packed(fields, torch.empty((n, n_channels(fields)), dtype=torch.int8, device=device),
+                      torch.empty((n, packed_blocks(fields)), dtype=torch.uint8, device=device))
+
+
+def _need_packed(p: Packed, name: str, fields: FieldList, n: Optional[int] = None):
+    fields = _field_list(fields)
+    if _field_list(p.fields) != fields:
+        raise ValueError(f"{name} is a checkpoint of fields {tuple(p.fields)}, not {fields}")
+    n = p.q.shape[0] if n is None else n
+    _need(p.q, f"{name}.q", torch.int8, (n, n_channels(fields)))
+    _need(p.exps, f"{name}.exps", torch.uint8, (n, packed_blocks(fields)))
+    _here(p.q, p.exps)
+
+
+def _need_rows(t: torch.Tensor, name: str, channels: int, dtype=None, n: Optional[int] = None):
+    _need(t, name, dtype)
+    _dtype(t)
+    if t.dim() != 2 or t.shape[1] != channels or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}, {channels}], got {tuple(t.shape)}")
+    _here(t)
+
+
+def _need_params(t: Optional[torch.Tensor], name: str, fields: FieldList):
+    if t is not None:
+        _need(t, name, torch.float32, (sum(int(m) for _, m in fields),))
+        _here(t)
+
+
+def _rows(x: Union[torch.Tensor, Packed]) -> Rows:
+    if isinstance(x, Packed):
+        return Rows(x.q.data_ptr(), x.exps.data_ptr())
+    return Rows(0 if x is None else x.data_ptr(), None)
+
+
+def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if ws is None:
+        return torch.empty((max(need, 256),), dtype=torch.uint8, device=device)
+    _need(ws, "workspace", torch.uint8)
+    _here(ws)
+    if ws.numel() < need:
+        raise ValueError(f"workspace must hold {need} bytes, got {ws.numel()}")
+    return ws
+
+
+def _new_or(out: Optional[torch.Tensor], name: str, like: torch.Tensor, channels: int) -> torch.Tensor:
+    if out is None:
+        return torch.empty((like.shape[0], channels), dtype=like.dtype, device=like.device)
+    _need_rows(out, name, channels, like.dtype, like.shape[0])
+    return out
+
+
+def pack(fields: FieldList, x: torch.Tensor, stream=None) -> Packed:
+    """An 8-bit checkpoint of x [n, C]."""
+    fields = _field_list(fields)
+    _need_rows(x, "x", n_channels(fields))
+    with _on(stream):
+        p = Packed.empty(fields, x.shape[0], x.device)
+    f = make_fields(fields)
+    check(lib().ssconv_pack(byref(f), _ptr(x), _dtype(x), x.shape[0], _ptr(p.q), _ptr(p.exps), _stream(stream)),
+          "ssconv_pack")
+    return p
+
+
+def unpack(p: Packed, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values that a checkpoint stands for (exact in either type)."""
+    _need_packed(p, "p", p.fields)
+    if out is None:
+        with _on(stream):
+            out = torch.empty(p.shape, dtype=dtype, device=p.device)
+    _need_rows(out, "out", p.shape[1], dtype, p.shape[0])
+    f = make_fields(p.fields)
+    check(lib().ssconv_unpack(byref(f), _ptr(p.q), _ptr(p.exps), p.shape[0], _dtype(out), _ptr(out), _stream(stream)),
+          "ssconv_unpack")
+    return out
+
+
+def site_norm_forward(fields: FieldList, x: Union[torch.Tensor, Packed], gain: Optional[torch.Tensor] = None,
+                      eps: float = NORM_EPS, out: Optional[torch.Tensor] = None, checkpoint: bool = False,
+                      dtype: Optional[torch.dtype] = None, stream=None):
+    """ssconv_site_norm_forward: the norm of every site of x [n, C] (or of a checkpoint; ``dtype`` is then the
+    result's, bf16 unless given).  With ``checkpoint``: (y, checkpoint of x)."""
+    fields = _field_list(fields)
+    C = n_channels(fields)
+    _need_params(gain, "gain", fields)
+    if isinstance(x, Packed):
+        if checkpoint:
+            raise ValueError("x is a checkpoint already")
+        _need_packed(x, "x", fields)
+        dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
+        if out is None:
+            with _on(stream):
+                out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        _need_rows(out, "out", C, dtype, x.shape[0])
+    else:
+        _need_rows(x, "x", C)
+        if dtype is not None and dtype != x.dtype:
+            raise TypeError(f"the result of {x.dtype} rows is {x.dtype}, not {dtype}")
+        with _on(stream):
+            out = _new_or(out, "out", x, C)
+    with _on(stream):
+        p = Packed.empty(fields, x.shape[0], x.device) if checkpoint else None
+    f, r = make_fields(fields), _rows(x)
+    check(lib().ssconv_site_norm_forward(byref(f), byref(r), _dtype(out), x.shape[0], float(eps), _ptr(gain), _ptr(out),
+                                         _ptr(p.q if p else None), _ptr(p.exps if p else None), _stream(stream)),
+          "ssconv_site_norm_forward")
+    return (out, p) if checkpoint else out
+
+
+def site_norm_backward(fields: FieldList, x: Union[torch.Tensor, Packed], dy: torch.Tensor,
+                       gain: Optional[torch.Tensor] = None, eps: float = NORM_EPS,
+                       dres: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None):
+    """ssconv_site_norm_backward: (gradient of x plus dres, gradient of the gain or None without one)."""
+    fields = _field_list(fields)
+    C = n_channels(fields)
+    _need_rows(dy, "dy", C)
+    n = dy.shape[0]
+    if isinstance(x, Packed):
+        _need_packed(x, "x", fields, n)
+    else:
+        _need_rows(x, "x", C, dy.dtype, n)
+    if dres is not None:
+        _need_rows(dres, "dres", C, dy.dtype, n)
+    _need_params(gain, "gain", fields)
+    f, r = make_fields(fields), _rows(x)
+    with _on(stream):
+        out = _new_or(out, "out", dy, C)
+        dgain = torch.empty_like(gain) if gain is not None else None
+        need = lib().ssconv_site_norm_workspace_size(byref(f), n) if gain is not None else 0
+        ws = _workspace(workspace, need, dy.device)
+    check(lib().ssconv_site_norm_backward(byref(f), byref(r), _ptr(dy), _ptr(dres), _dtype(dy), n, float(eps),
+                                          _ptr(gain), _ptr(out), _ptr(dgain), _ptr(ws), ws.numel(), _stream(stream)),
+          "ssconv_site_norm_backward")
+    return out, dgain
+
+
+def residual_forward(fields: FieldList, y: torch.Tensor, h: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                     gain_post: Optional[torch.Tensor] = None, gain_next: Optional[torch.Tensor] = None,
+                     eps: float = NORM_EPS, next_norm: bool = True, checkpoint: bool = False,
+                     out: Optional[torch.Tensor] = None, stream=None):
+    """ssconv_residual_forward: (h_out, x_out, checkpoint of y, checkpoint of h_out) of the convolution output y
+    [n, C + G] and the residual stream h [n, C]; x_out is None without ``next_norm``, the checkpoints without
+    ``checkpoint`` (and the one of h_out without ``next_norm``, whose backward alone reads it).  ``out`` may be h."""
+    fields = _field_list(fields)
+    full, C = gate_fields(fields), n_channels(fields)
+    _need_rows(h, "h", C)
+    n = h.shape[0]
+    _need_rows(y, "y", n_channels(full), h.dtype, n)
+    _need_params(scale, "scale", fields)
+    _need_params(gain_post, "gain_post", full)
+    _need_params(gain_next, "gain_next", fields)
+    if gain_next is not None and not next_norm:
+        raise ValueError("gain_next without the next norm")
+    with _on(stream):
+        h_out = _new_or(out, "out", h, C)
+        x_out = torch.empty_like(h) if next_norm else None
+        yp = Packed.empty(full, n, h.device) if checkpoint else None
+        hp = Packed.empty(fields, n, h.device) if checkpoint and next_norm else None
+    f = make_fields(fields)
+    check(lib().ssconv_residual_forward(byref(f), _ptr(y), _ptr(h), _dtype(h), n, float(eps), _ptr(gain_post),
+                                        _ptr(scale), _ptr(gain_next), _ptr(h_out), _ptr(x_out),
+                                        _ptr(yp.q if yp else None), _ptr(yp.exps if yp else None),
+                                        _ptr(hp.q if hp else None), _ptr(hp.exps if hp else None), _stream(stream)),
+          "ssconv_residual_forward")
+    return h_out, x_out, yp, hp
+
+
+def residual_backward(fields: FieldList, y: Union[torch.Tensor, Packed],
+                      h_out: Optional[Union[torch.Tensor, Packed]], dh: torch.Tensor,
+                      dx: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                      gain_post: Optional[torch.Tensor] = None, gain_next: Optional[torch.Tensor] = None,
+                      eps: float = NORM_EPS, workspace: Optional[torch.Tensor] = None, stream=None):
+    """ssconv_residual_backward: (dy, gradient of h, dscale, dgain_post, dgain_next) from the gradients dh of h_out and
+    dx of x_out (None without the next norm; h_out may then be None); y and h_out as rows or as checkpoints.  The
+    gradient of a parameter that is None is None."""
+    fields = _field_list(fields)
+    full, C = gate_fields(fields), n_channels(fields)
+    _need_rows(dh, "dh", C)
+    n, S = dh.shape[0], n_channels(full)
+    if isinstance(y, Packed):
+        _need_packed(y, "y", full, n)
+    else:
+        _need_rows(y, "y", S, dh.dtype, n)
+    if dx is not None:
+        _need_rows(dx, "dx", C, dh.dtype, n)
+        if h_out is None:
+            raise ValueError("dx needs h_out")
+        if isinstance(h_out, Packed):
+            _need_packed(h_out, "h_out", fields, n)
+        else:
+            _need_rows(h_out, "h_out", C, dh.dtype, n)
+    elif gain_next is not None:
+        raise ValueError("gain_next without dx")
+    _need_params(scale, "scale", fields)
+    _need_params(gain_post, "gain_post", full)
+    _need_params(gain_next, "gain_next", fields)
+    f, yr, hr = make_fields(fields), _rows(y), _rows(h_out)
+    with _on(stream):
+        dy = torch.empty((n, S), dtype=dh.dtype, device=dh.device)
+        dh_in = torch.empty_like(dh)
+        grads = [torch.empty_like(p) if p is not None else None for p in (scale, gain_post, gain_next)]
+        need = lib().ssconv_residual_workspace_size(byref(f), n) if any(g is not None for g in grads) else 0
+        ws = _workspace(workspace, need, dh.device)
+    check(lib().ssconv_residual_backward(byref(f), byref(yr), byref(hr), _ptr(dh), _ptr(dx), _dtype(dh), n, float(eps),
+                                         _ptr(gain_post), _ptr(scale), _ptr(gain_next), _ptr(dy), _ptr(dh_in),
+                                         _ptr(grads[1]), _ptr(grads[0]), _ptr(grads[2]), _ptr(ws), ws.numel(),
+                                         _stream(stream)), "ssconv_residual_backward")
+    return (dy, dh_in, *grads)
+
+
+def backward_packed_workspace_size(rb: Rulebook, dtype: torch.dtype, cin: int, cout: int) -> int:
+    return lib().ssconv_backward_packed_workspace_size(rb.handle, BF16 if dtype == torch.bfloat16 else F32, cin, cout)
+
+
+def backward_packed(feats: Packed, grad_out: torch.Tensor, rb: Rulebook, W: torch.Tensor,
+                    desc: Optional[BasisDesc] = None, basis: Optional[torch.Tensor] = None, norm: bool = False,
+                    gain: Optional[torch.Tensor] = None, eps: float = NORM_EPS, need_feats: bool = True,
+                    need_coeffs: bool = True, n_coeff: Optional[int] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None):
+    """ssconv_backward_packed: ``backward`` of a convolution whose input is the checkpoint ``feats`` (``norm``: the site
+    norm of it, with ``gain``)."""
+    fields = _field_list(feats.fields)
+    _need_packed(feats, "feats", fields, rb.n_in)
+    _need(W, "W", grad_out.dtype)
+    if W.dim() != 3 or W.shape[0] != rb.K or W.shape[2] != n_channels(fields):
+        raise ValueError(f"W must be [{rb.K}, cout, {n_channels(fields)}], got {tuple(W.shape)}")
+    K, cout, cin = W.shape
+    _need_rows(grad_out, "grad_out", cout, None, rb.n_out)
+    _need_params(gain, "gain", fields)
+    if gain is not None and not norm:
+        raise ValueError("gain without the norm")
+    coeffs = 0
+    if need_coeffs:
+        if desc is None or basis is None:
+            raise ValueError("desc and basis are required for the coefficient gradient")
+        floats, coeffs = basis_info(desc)
+        if n_coeff is not None and n_coeff != coeffs:
+            raise ValueError(f"the layer has {coeffs} coefficients, not {n_coeff}")
+        _need(basis, "basis", torch.float32)
+        if basis.numel() < floats:
+            raise ValueError(f"basis needs {floats} floats")
+    _here(W, grad_out, basis)
+    with _on(stream):
+        gf = torch.empty((rb.n_in, cin), dtype=grad_out.dtype, device=grad_out.device) if need_feats else None
+        gc = torch.empty((coeffs,), dtype=torch.float32, device=grad_out.device) if need_coeffs else None
+        ws = _workspace(workspace, backward_packed_workspace_size(rb, grad_out.dtype, cin, cout), grad_out.device)
+    f = make_fields(fields)
+    check(lib().ssconv_backward_packed(byref(f), _ptr(feats.q), _ptr(feats.exps), int(bool(norm)), float(eps),
+                                       _ptr(gain), _ptr(grad_out), _dtype(grad_out), cout, rb.handle, _ptr(W),
+                                       byref(desc) if desc is not None else None, _ptr(basis), _ptr(gf), _ptr(gc),
+                                       _ptr(ws), ws.numel(), _stream(stream)), "ssconv_backward_packed")
+    return gf, gc
 
 
 def pool_forward(feats: torch.Tensor, rb: Rulebook, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:

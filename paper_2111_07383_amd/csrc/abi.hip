@@ -4,6 +4,7 @@
 
 #include "conv.hpp"
 #include "norm.hpp"
+#include "site.hpp"
 #include "split_guard.hpp"
 #include "synth.hpp"
 
@@ -179,4 +180,50 @@ extern "C" int ssconv_backward(const void* feats, const void* grad_out, ssconv_d
     if (rc == SSCONV_OK) rc = jr;
   }
   return rc;
+}
+
+// ---------------------------------------------------------------------------
+// the gradient of a convolution whose input is kept as an 8-bit checkpoint
+// ---------------------------------------------------------------------------
+namespace {
+size_t packed_rows_bytes(const ssconv_rulebook* rb, ssconv_dtype dtype, int cin) {
+  return ((size_t)rb->n_in * cin * dtype_bytes(dtype) + 255) / 256 * 256;
+}
+}  // namespace
+
+extern "C" size_t ssconv_backward_packed_workspace_size(ssconv_rulebook_t rb, ssconv_dtype dtype, int cin, int cout) {
+  const size_t b = ssconv_backward_workspace_size(rb, dtype, cin, cout);
+  return b == 0 ? 0 : b + packed_rows_bytes(rb, dtype, cin);
+}
+
+// The rows are expanded in front of the kernel gradient rather than in its loads: a row is read by about
+// n_pairs / n_in pairs of every unit's lists, and would be normed and rounded that often.
+extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8_t* q, const uint8_t* exps, int norm,
+                                      double eps, const float* gain, const void* grad_out, ssconv_dtype dtype, int cout,
+                                      ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc,
+                                      const float* basis, void* grad_feats, float* grad_coeffs, void* workspace,
+                                      size_t ws_bytes, hipStream_t stream) {
+  SiteTab t;
+  SSC_TRY(make_sitetab(fields_in, false, &t));
+  if (norm && (!(eps > 0.0) || !((float)eps > 0.f) || !(eps < 1e30)))
+    return fail(SSCONV_E_INVALID, "eps must be positive and finite in fp32");
+  if (!norm && gain) return fail(SSCONV_E_INVALID, "gain without the norm");
+  SSC_TRY(check_conv_args(nullptr, grad_out, dtype, t.C, cout, rb, W));
+  SSC_TRY(rulebook_settle(rb));
+  if (rb->n_in > 0 && (!q || !exps)) return fail(SSCONV_E_INVALID, "NULL checkpoint");
+  const size_t need = ssconv_backward_packed_workspace_size(rb, dtype, t.C, cout);
+  if (!workspace || ws_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return fail(SSCONV_E_INVALID, "workspace must be 256-byte aligned and hold %zu bytes", need);
+  if (rb->n_out > 0 && !grad_out) return fail(SSCONV_E_INVALID, "NULL input buffer");
+  void* rows = workspace;
+  const size_t used = packed_rows_bytes(rb, dtype, t.C);
+  if (grad_coeffs && rb->n_in > 0) {
+    if (norm)
+      SSC_TRY(launch_site_norm_fwd(t, ssconv_rows{q, exps}, dtype, rb->n_in, (float)eps, gain, rows, nullptr, nullptr,
+                                   stream));
+    else
+      SSC_TRY(launch_unpack(t, q, exps, rb->n_in, dtype, rows, stream));
+  }
+  return ssconv_backward(rows, grad_out, dtype, t.C, cout, rb, W, desc, basis, grad_feats, grad_coeffs,
+                         (char*)workspace + used, ws_bytes - used, stream);
 }

@@ -1,0 +1,174 @@
+"""8-bit checkpoints on the GPU: the same bytes as the oracle's for every input, and the gradients of a convolution
+whose input is kept as one against those of the same values as rows, and against the fp64 oracle."""
+import numpy as np
+import pytest
+
+from cases import coords_of, layers_of, rel_err
+from oracle import conv as oc
+from oracle import rulebook as orb
+from oracle import site as os_
+from workloads import CONFIGS
+from workloads.configs import LayerSpec, gate_fields
+from workloads.gen import round_bf16
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+P = pytest.importorskip("paper_2111_07383_amd")
+from paper_2111_07383_amd.stack import Stack  # noqa: E402
+
+DEV = "cuda:0"
+FIELDS = [((0, 1),), ((0, 3), (1, 2)), ((0, 13), (1, 11), (2, 5)), ((0, 32), (1, 32), (2, 16)), ((0, 33), (4, 7)),
+          ((0, 1024),), ((0, 500), (1, 100), (2, 10)), ((0, 3), (1, 2)) * 4]
+
+
+def channels(f):
+    return sum(m * (2 * l + 1) for l, m in f)
+
+
+def dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(DEV, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 5, 4099])
+@pytest.mark.parametrize("f", FIELDS)
+def test_pack_bytes(f, n, dtype):
+    C, rng = channels(f), np.random.default_rng(n)
+    x = (rng.standard_normal((n, C)) * np.exp2(rng.integers(-20, 20, (n, 1)))).astype(np.float32)
+    if n > 1:
+        x[1:n:7] *= np.float32(2.0 ** -118)      # steps at the smallest scale, and values under it
+        x[2:n:11] = 0
+        x[3:n:13] = np.float32(3.3e38) * np.sign(x[3:n:13])
+        x[4:n:17, 0] = [np.nan, np.inf, -np.inf][n % 3]
+        x[0, :min(C, 4)] = np.array([127, 127.5, -63.25, 0.5], np.float32)[:min(C, 4)]   # ties and the clamp's border
+    if dtype == torch.bfloat16:
+        x = dev(x, dtype).float().cpu().numpy()
+    p = P.pack(f, dev(x, dtype))
+    q, e = os_.pack(f, x)
+    assert np.array_equal(p.exps.cpu().numpy(), e)
+    assert np.array_equal(p.q.cpu().numpy(), q)
+    want = os_.unpack(f, q, e)
+    for t in (torch.float32, torch.bfloat16):
+        np.testing.assert_array_equal(P.unpack(p, t).double().cpu().numpy(), want)   # exact in both
+    assert P.packed_blocks(f) == e.shape[1] and p.nbytes == q.size + e.size
+
+
+def test_unpack_any_bytes():
+    """Every exponent byte and every int8 value, as a caller could store them."""
+    f = ((0, 256),)
+    q = torch.arange(-128, 128, dtype=torch.int8, device=DEV).repeat(256, 1).contiguous()
+    e = torch.arange(256, dtype=torch.int32, device=DEV).to(torch.uint8)[:, None].repeat(1, 8).contiguous()
+    got = P.unpack(P.Packed(f, q, e), torch.float32).double().cpu().numpy()
+    with np.errstate(over="ignore"):
+        want = os_.unpack(f, q.cpu().numpy(), e.cpu().numpy()).astype(np.float32).astype(np.float64)
+    want[0] = 0                                   # no pack makes this byte: reads as a scale of zero
+    np.testing.assert_array_equal(got, want)
+
+
+def random_sites(rng, n, grid, batch=1):
+    c = np.stack([rng.integers(0, batch, n)] + [rng.integers(0, grid, n) for _ in range(3)], 1)
+    return np.unique(c, axis=0).astype(np.int32)
+
+
+CONV = {
+    "f104_k3_f32": (((0, 16), (1, 16), (2, 8)), 3, torch.float32, 900, 12),
+    "f208_k3_bf16": (((0, 32), (1, 32), (2, 16)), 3, torch.bfloat16, 1500, 14),
+    "ragged_k5_bf16": (((0, 13), (1, 11), (2, 5)), 5, torch.bfloat16, 400, 9),
+    "tiny_k3_f32": (((0, 2), (1, 2)), 3, torch.float32, 60, 6),
+    "one_site_f32": (((0, 4), (1, 1)), 3, torch.float32, 1, 4),
+}
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("name", list(CONV))
+def test_backward_packed(name, norm):
+    f, ks, dtype, n, grid = CONV[name]
+    rng = np.random.default_rng(n)
+    coords = random_sites(rng, n, grid)
+    n, C, fo = len(coords), channels(f), gate_fields(f)
+    spec = LayerSpec(ks, 1, True, f, fo, shells=tuple(float(i) for i in range(ks // 2 + 1)), gated=True)
+    lay = oc.Layer(spec)
+    w = rng.standard_normal(lay.n_coeff) / (C * ks ** 3) ** 0.5
+    bf16 = dtype == torch.bfloat16
+    kappa = lay.kappa(w, bf16=bf16)
+    x = rng.standard_normal((n, C)).astype(np.float32)
+    g = rng.standard_normal((n, spec.cout)).astype(np.float32)
+    gain = (1 + 0.2 * rng.standard_normal(sum(m for _, m in f))).astype(np.float32)
+    if bf16:
+        x, g = round_bf16(x), round_bf16(g)
+    desc = P.layer_desc(spec)
+    basis = torch.from_numpy(P.basis_build(desc)).to(DEV)
+    rb = P.Rulebook(torch.from_numpy(coords).to(DEV), grid, ks, 1, True)
+    W = P.synth_kernel(desc, basis, dev(w), dtype)
+    p = P.pack(f, dev(x, dtype))
+    kw = dict(norm=True, gain=dev(gain), eps=1e-5) if norm else {}
+    gf, gc = P.backward_packed(p, dev(g, dtype), rb, W, desc, basis, **kw)
+    # the same bits as the rows that the checkpoint stands for
+    rows = P.site_norm_forward(f, p, dev(gain), 1e-5, dtype=dtype) if norm else P.unpack(p, dtype)
+    rf, rc = P.backward(rows, dev(g, dtype), rb, W, desc, basis)
+    assert torch.equal(gf, rf) and torch.equal(gc, rc)
+    # the oracle at the checkpoint's values; the package's own bounds, L_inf error over L_inf norm
+    v = os_.unpack(f, *os_.pack(f, x))
+    if norm:
+        v = os_.norm_forward(f, v, gain)
+        v = round_bf16(v.astype(np.float32)) if bf16 else v
+    R = orb.rulebook(coords, coords, ks, 1)
+    dk = oc.grad_kappa(v, g, R, kappa.shape)
+    assert rel_err(gc.cpu().numpy(), oc.synth_adjoint(spec, lay.basis, dk)) < (2e-2 if bf16 else 1e-4)
+    assert rel_err(gf.float().cpu().numpy(), oc.grad_feats(g, R, kappa, n)) < (2e-2 if bf16 else 1e-4)
+    # either gradient alone, and a caller's workspace
+    ws = torch.empty(P.backward_packed_workspace_size(rb, dtype, C, spec.cout), dtype=torch.uint8, device=DEV)
+    only, none = P.backward_packed(p, dev(g, dtype), rb, W, need_coeffs=False, workspace=ws, **kw)
+    assert torch.equal(only, gf) and none is None
+    none, only = P.backward_packed(p, dev(g, dtype), rb, W, desc, basis, need_feats=False, workspace=ws, **kw)
+    assert torch.equal(only, gc) and none is None
+    with pytest.raises(ValueError):
+        P.backward_packed(p, dev(g, dtype), rb, W, desc, basis, workspace=ws[:-1], **kw)
+    with pytest.raises(ValueError):
+        P.backward_packed(p, dev(g, dtype), rb, W, desc, basis, gain=dev(gain))      # a gain without the norm
+    with pytest.raises(ValueError):
+        P.backward_packed(P.pack(((0, C),), dev(x, dtype)), dev(g[:-1] if n > 1 else g[:, :-1], dtype), rb, W, desc, basis)
+    rb.close()
+
+
+def test_backward_packed_no_sites():
+    f = ((0, 2), (1, 1))
+    spec = LayerSpec(3, 1, True, f, gate_fields(f), shells=(0.0, 1.0))
+    desc = P.layer_desc(spec)
+    basis = torch.from_numpy(P.basis_build(desc)).to(DEV)
+    rb = P.Rulebook(torch.zeros((0, 4), dtype=torch.int32, device=DEV), 8, 3, 1, True)
+    W = torch.ones((27, 6, 5), device=DEV)
+    p = P.Packed.empty(f, 0, DEV)
+    gf, gc = P.backward_packed(p, torch.zeros((0, 6), device=DEV), rb, W, desc, basis)
+    assert gf.shape == (0, 5) and bool((gc == 0).all())
+    rb.close()
+
+
+def test_stack_with_checkpoints():
+    """The five-layer stack keeps checkpoints: the forward's bits are those of the plain stack, and every gradient is
+    the composition of the package's calls at the checkpoints' values."""
+    spec = CONFIGS[5]
+    Ls = layers_of(5)
+    coords = torch.from_numpy(coords_of(5)).to(DEV)
+    rng = np.random.default_rng(3)
+    feats = dev(rng.standard_normal((len(coords), 8)))
+    a = Stack.create(spec.layers, [L.coeffs for L in Ls], spec.grid, DEV)
+    b = Stack.create(spec.layers, [L.coeffs for L in Ls], spec.grid, DEV, checkpoint=True)
+    ca, ha = a.forward(coords, feats)
+    cb, hb = b.forward(coords, feats)
+    assert torch.equal(ca, cb) and torch.equal(ha, hb)
+    g = dev(rng.standard_normal(ha.shape))
+    gi, gcs = b.backward(g)
+    for i in range(len(a.layers) - 1, -1, -1):
+        La, Lb, s = a.layers[i], b.layers[i], a.layers[i].layer
+        assert isinstance(Lb.x, P.Packed) and (Lb.y is None or isinstance(Lb.y, P.Packed))
+        assert torch.equal(Lb.x.q, P.pack(s.fields_in, La.x).q)
+        if s.gated:
+            g = P.gate_backward(s.fields_out[:-1], P.unpack(P.pack(s.fields_out, La.y), torch.float32), g)
+        x = P.unpack(P.pack(s.fields_in, La.x), torch.float32)
+        g, gc = P.backward(x, g, La.rb, La.W, La.desc, La.basis)
+        assert torch.equal(gc, gcs[i])
+    assert torch.equal(g, gi)
+    a.close()
+    b.close()

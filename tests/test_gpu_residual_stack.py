@@ -1,0 +1,160 @@
+"""The residual trunk: norm, convolution and block tail together, with and without checkpoints, against the fp64
+oracle and against differences of its own forward."""
+import numpy as np
+import pytest
+
+from cases import rel_err
+from oracle import conv as oc
+from oracle import rulebook as orb
+from oracle import site as os_
+from workloads.configs import LayerSpec, gate_fields
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+P = pytest.importorskip("paper_2111_07383_amd")
+from paper_2111_07383_amd.stack import ResidualStack  # noqa: E402
+
+DEV = "cuda:0"
+EPS = 1e-5
+F = ((0, 9), (1, 6), (2, 3))
+C = 9 + 18 + 15
+
+
+def setup(dtype, checkpoint, ksizes=(3, 5, 3), n=400, seed=0):
+    rng = np.random.default_rng(seed)
+    c = np.stack([rng.integers(0, 2, n)] + [rng.integers(0, 9, n) for _ in range(3)], 1)
+    coords = np.unique(c, axis=0).astype(np.int32)
+    specs = [LayerSpec(k, 1, True, F, gate_fields(F), shells=tuple(float(i) for i in range(k // 2 + 1)), gated=True)
+             for k in ksizes]
+    lays = [oc.Layer(s) for s in specs]
+    ws = [(rng.standard_normal(L.n_coeff) / (C * s.ksize ** 3) ** 0.5 * 3).astype(np.float32) for s, L in zip(specs, lays)]
+    st = ResidualStack.create(specs, ws, 9, DEV, dtype, scale=0.4, checkpoint=checkpoint)
+    for i in range(len(specs)):
+        for p in (st.scale[i], st.gain_pre[i], st.gain_post[i]):
+            p.mul_(torch.from_numpy(1 + 0.2 * rng.standard_normal(p.numel())).float().to(DEV))
+    feats = torch.from_numpy(rng.standard_normal((len(coords), C))).to(DEV, dtype)
+    grad = torch.from_numpy(rng.standard_normal((len(coords), C))).to(DEV, dtype)
+    return st, specs, lays, ws, coords, feats, grad
+
+
+def oracle_forward(st, specs, lays, ws, coords, feats):
+    """(stream in front of every block and behind the last, conv inputs, conv outputs)."""
+    p = lambda t: t.double().cpu().numpy()  # noqa: E731
+    h, hs, xs, ys, Rs, ks = p(feats), [], [], [], [], []
+    for i, s in enumerate(specs):
+        Rs.append(orb.rulebook(coords, coords, s.ksize, 1))
+        ks.append(lays[i].kappa(ws[i].astype(np.float64)))
+        hs.append(h)
+        xs.append(os_.norm_forward(F, h, p(st.gain_pre[i]), EPS))
+        ys.append(oc.forward(xs[-1], Rs[-1], ks[-1], len(h)))
+        h = os_.residual_forward(F, ys[-1], h, p(st.scale[i]), p(st.gain_post[i]), EPS)
+    return hs + [h], xs, ys, Rs, ks
+
+
+def test_against_oracle_fp32():
+    st, specs, lays, ws, coords, feats, grad = setup(torch.float32, False)
+    out = st.forward(torch.from_numpy(coords).to(DEV), feats)
+    hs, xs, ys, Rs, ks = oracle_forward(st, specs, lays, ws, coords, feats)
+    assert rel_err(out.cpu().numpy(), hs[-1]) < 1e-4
+    dfeats, g = st.backward(grad)
+    p = lambda t: t.double().cpu().numpy()  # noqa: E731
+    dh, dx = p(grad), None
+    for i in range(len(specs) - 1, -1, -1):
+        y = ys[i]
+        dy, dh, dsc, dpo, dne = os_.residual_backward(
+            F, y, hs[i + 1], dh, dx, p(st.scale[i]), p(st.gain_post[i]), None if dx is None else p(st.gain_pre[i + 1]), EPS)
+        # the sign of a scalar is a decision; no value here lies within the forward's error of its border
+        u = os_.norm_forward(gate_fields(F), y, p(st.gain_post[i]), EPS)[:, :9]
+        ug = os_.norm_forward(gate_fields(F), p(st.blocks[i].y), p(st.gain_post[i]), EPS)[:, :9]
+        assert np.array_equal(u > 0, ug > 0)
+        assert rel_err(p(g["scale"][i]), dsc) < 1e-4 and rel_err(p(g["gain_post"][i]), dpo) < 1e-4
+        if dne is not None:
+            assert rel_err(p(g["gain_pre"][i + 1]), dne) < 1e-4
+        dk = oc.grad_kappa(xs[i], dy, Rs[i], ks[i].shape)
+        assert rel_err(p(g["coeffs"][i]), oc.synth_adjoint(specs[i], lays[i].basis, dk)) < 1e-4
+        dx = oc.grad_feats(dy, Rs[i], ks[i], len(coords))
+    back, dg0 = os_.norm_backward(F, hs[0], dx, p(st.gain_pre[0]), EPS)
+    assert rel_err(p(g["gain_pre"][0]), dg0) < 1e-4
+    assert rel_err(p(dfeats), dh + back) < 1e-4
+    st.close()
+
+
+def test_gradients_against_differences():
+    """Central differences of <out, grad> along the gradient itself, block by block and parameter by parameter: the
+    fp32 forward is off by about 1e-6 of a value, so a step that moves the result by 1e-2 of it gives three digits."""
+    st, specs, lays, ws, coords, feats, grad = setup(torch.float32, False, ksizes=(3, 3), seed=5)
+    ct = torch.from_numpy(coords).to(DEV)
+    st.forward(ct, feats)
+    dfeats, g = st.backward(grad)
+    g = {k: [t.clone() for t in v] for k, v in g.items()}
+
+    def loss():
+        return float((st.forward(ct, feats).double() * grad.double()).sum())
+
+    targets = [(feats, dfeats)]
+    for i in range(2):
+        targets += [(st.scale[i], g["scale"][i]), (st.gain_pre[i], g["gain_pre"][i]),
+                    (st.gain_post[i], g["gain_post"][i]), (st.blocks[i].coeffs, g["coeffs"][i])]
+    for t, d in targets:
+        step = d / d.norm() * 2e-3 * t.norm()
+        keep = t.clone()
+        t.copy_(keep + step)
+        a, da = loss(), (t - keep).double()
+        t.copy_(keep - step)
+        b, db = loss(), (t - keep).double()
+        t.copy_(keep)
+        want = float(((da - db) * d.double()).sum())
+        # third derivatives and relu borders that the step crosses: 2e-2 of the difference
+        assert abs((a - b) - want) <= 2e-2 * abs(want)
+    st.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_checkpoints(dtype):
+    """With checkpoints the forward's bits stay, and the backward is the composition of the calls at the kept values."""
+    st, specs, lays, ws, coords, feats, grad = setup(dtype, True, seed=7)
+    plain = setup(dtype, False, seed=7)[0]
+    ct = torch.from_numpy(coords).to(DEV)
+    out = st.forward(ct, feats)
+    assert torch.equal(out, plain.forward(ct, feats))
+    assert all(isinstance(h, P.Packed) for h in st.h) and all(L.x is None and isinstance(L.y, P.Packed) for L in st.blocks)
+    dfeats, g = st.backward(grad)
+    dh, dx = grad, None
+    for i in range(2, -1, -1):
+        L = plain.blocks[i]
+        y = P.pack(gate_fields(F), L.y)
+        h = P.pack(F, plain.h[i + 1]) if i < 2 else None
+        dy, dh, dsc, dpo, dne = P.residual_backward(F, y, h, dh, dx, st.scale[i], st.gain_post[i],
+                                                    st.gain_pre[i + 1] if i < 2 else None, EPS)
+        assert torch.equal(dsc, g["scale"][i]) and torch.equal(dpo, g["gain_post"][i])
+        x = P.site_norm_forward(F, P.pack(F, plain.h[i]), st.gain_pre[i], EPS, dtype=dtype)
+        dx, gc = P.backward(x, dy, L.rb, L.W, L.desc, L.basis)
+        assert torch.equal(gc, g["coeffs"][i])
+    want, dg = P.site_norm_backward(F, P.pack(F, feats), dx, st.gain_pre[0], EPS, dres=dh)
+    assert torch.equal(want, dfeats) and torch.equal(dg, g["gain_pre"][0])
+    kept = sum(h.nbytes for h in st.h) + sum(L.y.nbytes for L in st.blocks)
+    rows = sum(t.numel() * t.element_size() for t in plain.h + [L.y for L in plain.blocks] + [L.x for L in plain.blocks])
+    assert kept < 0.45 * rows
+    st.close()
+    plain.close()
+
+
+def test_refusals_and_empty():
+    with pytest.raises(ValueError):
+        ResidualStack.create([LayerSpec(3, 2, False, F, gate_fields(F), shells=(0.0, 1.0), gated=True)], [None], 9, DEV)
+    with pytest.raises(ValueError):
+        ResidualStack.create([LayerSpec(3, 1, True, F, F, shells=(0.0, 1.0), gated=True)], [None], 9, DEV)
+    none = ResidualStack.create([], [], 9, DEV)
+    x = torch.ones((3, C), device=DEV)
+    assert none.forward(torch.zeros((3, 4), dtype=torch.int32, device=DEV), x) is x
+    st, specs, lays, ws, coords, feats, grad = setup(torch.float32, True)
+    out = st.forward(torch.zeros((0, 4), dtype=torch.int32, device=DEV), feats[:0])
+    assert out.shape == (0, C)
+    d, g = st.backward(out)
+    assert d.shape == (0, C) and all(bool((t == 0).all()) for v in g.values() for t in v)
+    one = np.array([[0, 4, 4, 4]], np.int32)          # a single site, as a tracker's smallest call
+    out = st.forward(torch.from_numpy(one).to(DEV), feats[:1].contiguous())
+    hs = oracle_forward(st, specs, lays, ws, one, feats[:1])[0]
+    assert rel_err(out.cpu().numpy(), hs[-1]) < 1e-4
+    st.close()
