@@ -205,8 +205,7 @@ extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8
                                       size_t ws_bytes, hipStream_t stream) {
   SiteTab t;
   SSC_TRY(make_sitetab(fields_in, false, &t));
-  if (norm && (!(eps > 0.0) || !((float)eps > 0.f) || !(eps < 1e30)))
-    return fail(SSCONV_E_INVALID, "eps must be positive and finite in fp32");
+  if (norm) SSC_TRY(check_site_eps(eps));
   if (!norm && gain) return fail(SSCONV_E_INVALID, "gain without the norm");
   SSC_TRY(check_conv_args(nullptr, grad_out, dtype, t.C, cout, rb, W));
   SSC_TRY(rulebook_settle(rb));
@@ -217,13 +216,8 @@ extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8
   if (rb->n_out > 0 && !grad_out) return fail(SSCONV_E_INVALID, "NULL input buffer");
   void* rows = workspace;
   const size_t used = packed_rows_bytes(rb, dtype, t.C);
-  if (grad_coeffs && rb->n_in > 0) {
-    if (norm)
-      SSC_TRY(launch_site_norm_fwd(t, ssconv_rows{q, exps}, dtype, rb->n_in, (float)eps, gain, rows, nullptr, nullptr,
-                                   stream));
-    else
-      SSC_TRY(launch_unpack(t, q, exps, rb->n_in, dtype, rows, stream));
-  }
+  if (grad_coeffs && rb->n_in > 0)
+    SSC_TRY(expand_packed(t, dtype, q, exps, rb->n_in, norm != 0, (float)eps, gain, rows, stream));
   return ssconv_backward(rows, grad_out, dtype, t.C, cout, rb, W, desc, basis, grad_feats, grad_coeffs,
                          (char*)workspace + used, ws_bytes - used, stream);
 }

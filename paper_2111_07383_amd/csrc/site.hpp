@@ -1,14 +1,19 @@
 // Norm of a site, tail of a residual block, 8-bit checkpoints: what the kernels and the entry points share.
 #pragma once
 
+#include <algorithm>
+
 #include "common.hpp"
 
 namespace ssconv {
 
 constexpr int kPackBlock = 32;  // channels that share an exponent
 constexpr int kSiteMaxC = 1024;
+constexpr int kChunk = 8;       // channels that a lane holds at a time
+constexpr int kSiteNT = 256;
 
-// Entries of a row (those of a field list, and behind them the gates of a residual block as one more).
+// Entries of a row (those of a field list, and behind them the gates of a residual block as one more).  Every entry is
+// cut into chunks of 8 channels of its own.
 struct SiteTab {
   int n;                            // entries
   int l[SSCONV_MAX_ENTRIES];
@@ -16,30 +21,77 @@ struct SiteTab {
   int ch0[SSCONV_MAX_ENTRIES + 1];  // first channel of each entry, ch0[n] = channels
   int f0[SSCONV_MAX_ENTRIES + 1];   // first field
   int b0[SSCONV_MAX_ENTRIES + 1];   // first checkpoint block, b0[n] = blocks of a row
+  int t0[SSCONV_MAX_ENTRIES + 1];   // first chunk, t0[n] = chunks of a row
   int gate0[SSCONV_MAX_ENTRIES];    // gate of the first field of each entry (entries of order > 0)
   int C, G;                         // channels without the gates, gates
+  int n_regular;                    // entries without the gates'
+  int ragged;                       // some entry is not a multiple of 8 channels
 };
 
 // gated: the gates of the fields of order > 0 as one more entry.
 int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t);
 
-// Exponent byte of a block with this largest magnitude (as bits), and its scale and the scale's inverse.
-__device__ __forceinline__ int pack_byte(uint32_t amax_bits) {
-  if (amax_bits >= 0x7f800000u) return 255;
-  const int k = (int)(amax_bits >> 23) - 127 - 6 + ((amax_bits & 0x7fffffu) > 0x7e0000u ? 1 : 0);  // 127/64 = 1 + 63/64
-  return (k < -126 ? -126 : k) + 127;
+// Lanes per row and chunks per lane: the fewest lanes that hold a row, one chunk each, or 64 lanes with three.
+inline int site_lanes(const SiteTab& t) {
+  const int c = t.t0[t.n];
+  return c <= 16 ? 16 : c <= 32 ? 32 : 64;
 }
-__device__ __forceinline__ float pack_scale(int byte) {
-  return byte == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)byte << 23);
+// Rows that a workgroup takes at a time.
+inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
+
+// Workgroups of a call: all rows at once where they are few, else as many as stay on the chip, which then loop.
+inline unsigned site_blocks(const SiteTab& t, int64_t n, int per_cu) {
+  const int64_t rows = site_rows(t);
+  return (unsigned)std::min<int64_t>((n + rows - 1) / rows, 256 * per_cu);
 }
-__device__ __forceinline__ float pack_inverse(int byte) {  // 2^-k; of a block with no value to keep 0
-  return byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23);
+constexpr int kFwdPerCu = 8;
+constexpr int kBwdPerCu = 4;  // each leaves a row of partial sums of the parameters' gradients
+
+struct NormArgs {
+  ssconv_rows x;
+  const void *dy, *dres;
+  int64_t n;
+  float eps;
+  const float* gain;
+  void* out;       // y, or dx
+  int8_t* q;       // checkpoint of x (forward)
+  uint8_t* exps;
+  float* part;     // [workgroups][C] (backward)
+};
+struct TailArgs {
+  ssconv_rows y, h;  // h: h_out in the backward
+  const void *dh, *dx;
+  int64_t n;
+  float eps;
+  const float *gain_post, *scale, *gain_next;
+  void *h_out, *x_out;  // forward
+  int8_t *yq, *hq;
+  uint8_t *ye, *he;
+  void *dy, *dh_in;  // backward
+  float* part;       // [workgroups][S + 2 C]: post, scale, next
+};
+
+int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st);
+int launch_norm_bwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st);
+int launch_tail_fwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStream_t st);
+int launch_tail_bwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStream_t st);
+int launch_pack(const SiteTab& t, ssconv_dtype dt, const void* x, int64_t n, int8_t* q, uint8_t* exps, hipStream_t st);
+int launch_unpack(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, void* x,
+                  hipStream_t st);
+
+// Rows of a checkpoint, or their site norm, for the gradient of a convolution (checked arguments).
+inline int expand_packed(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, bool norm,
+                         float eps, const float* gain, void* rows, hipStream_t st) {
+  if (!norm) return launch_unpack(t, dt, q, exps, n, rows, st);
+  NormArgs a{};
+  a.x = ssconv_rows{q, exps};
+  a.n = n;
+  a.eps = eps;
+  a.gain = gain;
+  a.out = rows;
+  return launch_norm_fwd(t, dt, a, st);
 }
 
-// Rows of the site norm of a checkpoint, for the gradient of the convolution behind it (checked arguments).
-int launch_site_norm_fwd(const SiteTab& t, const ssconv_rows& x, ssconv_dtype dt, int64_t n, float eps,
-                         const float* gain, void* y, int8_t* q, uint8_t* exps, hipStream_t st);
-int launch_unpack(const SiteTab& t, const int8_t* q, const uint8_t* exps, int64_t n, ssconv_dtype dt, void* x,
-                  hipStream_t st);
+int check_site_eps(double eps);
 
 }  // namespace ssconv

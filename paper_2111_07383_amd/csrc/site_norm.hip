@@ -1,0 +1,166 @@
+// Norm of a site, forward and backward (formulas in include/ssconv.h), and the 8-bit checkpoints.
+//
+// Bound: memory. A row is read and written once, 16 bytes a lane (site_row.hpp says how rows lie in registers).
+#include "site_row.hpp"
+
+namespace ssconv {
+namespace {
+
+template <typename T, int L, int K, bool RAG>
+__global__ __launch_bounds__(kSiteNT) void norm_fwd_kernel(SiteTab t, NormArgs a) {
+  using R = Row<L, K, RAG>;
+  R w;
+  w.init(t, t.n);
+  const int C = t.ch0[t.n], B = t.b0[t.n];
+  f8 g[K];
+  w.params(a.gain, g, t.n);
+  const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
+  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < a.n; r0 += step) {
+    const bool on = r0 + w.sub < a.n;
+    const int64_t row = on ? r0 + w.sub : a.n - 1;
+    f8 x[K];
+    float r[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      x[k] = a.x.exps ? w.load_packed((const int8_t*)a.x.data + row * C, a.x.exps + row * B, k)
+                      : w.template load<T>((const T*)a.x.data + row * C, k);
+    if (a.q) w.pack(x, a.q + row * C, a.exps + row * B, t.n, on);
+    w.norm(x, r, a.eps);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (on) w.template store<T>((T*)a.out + row * C, k, x[k] * g[k]);
+  }
+}
+
+template <typename T, int L, int K, bool RAG>
+__global__ __launch_bounds__(kSiteNT) void norm_bwd_kernel(SiteTab t, NormArgs a) {
+  extern __shared__ float lds[];
+  using R = Row<L, K, RAG>;
+  R w;
+  w.init(t, t.n);
+  const int C = t.ch0[t.n], B = t.b0[t.n];
+  f8 g[K], acc[K];
+  w.params(a.gain, g, t.n);
+#pragma unroll
+  for (int k = 0; k < K; ++k) acc[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
+  const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
+  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < a.n; r0 += step) {
+    const bool on = r0 + w.sub < a.n;
+    const int64_t row = on ? r0 + w.sub : a.n - 1;
+    f8 x[K], d[K], res[K];
+    float r[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      x[k] = a.x.exps ? w.load_packed((const int8_t*)a.x.data + row * C, a.x.exps + row * B, k)
+                      : w.template load<T>((const T*)a.x.data + row * C, k);
+      d[k] = w.template load<T>((const T*)a.dy + row * C, k);
+      res[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (a.dres) res[k] = w.template load<T>((const T*)a.dres + row * C, k);
+    }
+    w.norm(x, r, a.eps);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (on) acc[k] += d[k] * x[k];
+      d[k] *= g[k];
+    }
+    w.norm_back(x, r, d);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (on) w.template store<T>((T*)a.out + row * C, k, d[k] + res[k]);
+  }
+  if (a.part) sum_rows<L, K, RAG>(w, acc, C, lds, a.part + (int64_t)blockIdx.x * C);
+}
+
+template <typename T, int L, int K, bool RAG>
+__global__ __launch_bounds__(kSiteNT) void pack_kernel(SiteTab t, const T* x, int64_t n, int8_t* q, uint8_t* exps) {
+  using R = Row<L, K, RAG>;
+  R w;
+  w.init(t, t.n);
+  const int C = t.ch0[t.n], B = t.b0[t.n];
+  const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
+  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < n; r0 += step) {
+    const bool on = r0 + w.sub < n;
+    const int64_t row = on ? r0 + w.sub : n - 1;
+    f8 v[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = w.template load<T>(x + row * C, k);
+    w.pack(v, q + row * C, exps + row * B, t.n, on);
+  }
+}
+
+template <typename T, int L, int K, bool RAG>
+__global__ __launch_bounds__(kSiteNT) void unpack_kernel(SiteTab t, const int8_t* q, const uint8_t* exps, int64_t n,
+                                                         T* x) {
+  using R = Row<L, K, RAG>;
+  R w;
+  w.init(t, t.n);
+  const int C = t.ch0[t.n], B = t.b0[t.n];
+  const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
+  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < n; r0 += step) {
+    const int64_t row = r0 + w.sub;
+    if (row < n)
+#pragma unroll
+      for (int k = 0; k < K; ++k) w.template store<T>(x + row * C, k, w.load_packed(q + row * C, exps + row * B, k));
+  }
+}
+
+}  // namespace
+
+int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st) {
+  const unsigned nb = site_blocks(t, a.n, kFwdPerCu);
+  auto go = [&](auto kernel) {
+    kernel<<<nb, kSiteNT, 0, st>>>(t, a);
+    SSC_HIP(hipGetLastError());
+    return (int)SSCONV_OK;
+  };
+#define SSK_GO(L_, K_, R_) \
+  return dt == SSCONV_F32 ? go(norm_fwd_kernel<float, L_, K_, R_>) : go(norm_fwd_kernel<uint16_t, L_, K_, R_>)
+  SSK_SITE_DISPATCH(t, SSK_GO);
+#undef SSK_GO
+}
+
+int launch_norm_bwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st) {
+  const unsigned nb = site_blocks(t, a.n, kBwdPerCu);
+  const size_t lds = a.part ? (size_t)site_rows(t) * t.ch0[t.n] * 4 : 0;
+  auto go = [&](auto kernel) {
+    kernel<<<nb, kSiteNT, lds, st>>>(t, a);
+    SSC_HIP(hipGetLastError());
+    return (int)SSCONV_OK;
+  };
+#define SSK_GO(L_, K_, R_) \
+  return dt == SSCONV_F32 ? go(norm_bwd_kernel<float, L_, K_, R_>) : go(norm_bwd_kernel<uint16_t, L_, K_, R_>)
+  SSK_SITE_DISPATCH(t, SSK_GO);
+#undef SSK_GO
+}
+
+int launch_pack(const SiteTab& t, ssconv_dtype dt, const void* x, int64_t n, int8_t* q, uint8_t* exps,
+                hipStream_t st) {
+  const unsigned nb = site_blocks(t, n, kFwdPerCu);
+  auto go = [&](auto kernel, auto* p) {
+    kernel<<<nb, kSiteNT, 0, st>>>(t, p, n, q, exps);
+    SSC_HIP(hipGetLastError());
+    return (int)SSCONV_OK;
+  };
+#define SSK_GO(L_, K_, R_)                                                              \
+  return dt == SSCONV_F32 ? go(pack_kernel<float, L_, K_, R_>, (const float*)x)         \
+                          : go(pack_kernel<uint16_t, L_, K_, R_>, (const uint16_t*)x)
+  SSK_SITE_DISPATCH(t, SSK_GO);
+#undef SSK_GO
+}
+
+int launch_unpack(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, void* x,
+                  hipStream_t st) {
+  const unsigned nb = site_blocks(t, n, kFwdPerCu);
+  auto go = [&](auto kernel, auto* p) {
+    kernel<<<nb, kSiteNT, 0, st>>>(t, q, exps, n, p);
+    SSC_HIP(hipGetLastError());
+    return (int)SSCONV_OK;
+  };
+#define SSK_GO(L_, K_, R_)                                                      \
+  return dt == SSCONV_F32 ? go(unpack_kernel<float, L_, K_, R_>, (float*)x)     \
+                          : go(unpack_kernel<uint16_t, L_, K_, R_>, (uint16_t*)x)
+  SSK_SITE_DISPATCH(t, SSK_GO);
+#undef SSK_GO
+}
+
+}  // namespace ssconv

@@ -1,0 +1,443 @@
+// Rows of sites in registers: what the kernels of the site norm, the residual tail and the checkpoints share.
+//
+// A row is L lanes' of a wavefront (64 / L rows each), every lane holding K chunks of 8 channels of one entry each.
+// Loads and stores are one 16-byte access a chunk (bf16; two in fp32, 8 bytes of a checkpoint) at whatever alignment
+// the row has, so nothing passes through LDS but what lanes owe each other.  An entry that is no multiple of 8 ends in
+// a chunk moved back to its end: its first `lo` channels are the previous chunk's too, take part in no sum and are
+// computed and stored twice, with the same bits.  Entries under 8 channels have one chunk of `hi` channels, moved
+// element by element.
+//
+// With K = 1 an entry is a run of lanes, and its sums are a segmented prefix sum (4 to 6 DPP additions, whatever the
+// number of entries) of which the run's last lane is read back; with K = 3 (rows over 64 chunks) they are butterflies
+// entry by entry.
+#pragma once
+
+#include "site.hpp"
+
+namespace ssconv {
+
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef u4 u4_any __attribute__((aligned(2)));
+typedef f8 f8_any __attribute__((aligned(4)));
+typedef u2 u2_any __attribute__((aligned(1)));
+
+// Exponent byte of a block with this largest magnitude (as bits), and its scale and the scale's inverse.
+__device__ __forceinline__ int pack_byte(uint32_t amax_bits) {
+  const int k = (int)(amax_bits >> 23) - 127 - 6 + ((amax_bits & 0x7fffffu) > 0x7e0000u ? 1 : 0);  // 127/64 = 1 + 63/64
+  return amax_bits >= 0x7f800000u ? 255 : (k < -126 ? -126 : k) + 127;
+}
+__device__ __forceinline__ float pack_scale(int byte) {
+  return __uint_as_float(byte == 255 ? 0x7fc00000u : (uint32_t)byte << 23);
+}
+__device__ __forceinline__ float pack_inverse(int byte) {  // 2^-k; 0 for a block that keeps no value
+  return __uint_as_float(byte == 255 ? 0u : (uint32_t)(254 - byte) << 23);
+}
+
+// Order of LDS accesses of the lanes of one wavefront (the LDS itself serves a wavefront in order).
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or_0(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, true));
+}
+
+__device__ __forceinline__ float read_lane(float v, int addr) {
+  return __int_as_float(__builtin_amdgcn_ds_bpermute(addr, __float_as_int(v)));
+}
+
+template <typename T>
+__device__ __forceinline__ f8 load8(const T* p);
+template <>
+__device__ __forceinline__ f8 load8<float>(const float* p) {
+  return *reinterpret_cast<const f8_any*>(p);
+}
+template <>
+__device__ __forceinline__ f8 load8<uint16_t>(const uint16_t* p) {
+  const u4 v = *reinterpret_cast<const u4_any*>(p);
+  f8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = __uint_as_float(v[i] << 16);
+    r[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+  }
+  return r;
+}
+// The values as they are stored (rounded to nearest even), written to p where full.
+template <typename T>
+__device__ __forceinline__ f8 round8(f8 v);
+template <>
+__device__ __forceinline__ f8 round8<float>(f8 v) { return v; }
+template <>
+__device__ __forceinline__ f8 round8<uint16_t>(f8 v) {
+  return __builtin_convertvector(__builtin_convertvector(v, bf8), f8);
+}
+__device__ __forceinline__ void store8(float* p, f8 v) { *reinterpret_cast<f8_any*>(p) = v; }
+__device__ __forceinline__ void store8(uint16_t* p, f8 v) {
+  *reinterpret_cast<u4_any*>(p) = __builtin_bit_cast(u4, __builtin_convertvector(v, bf8));
+}
+
+template <int L, int K, bool RAG>
+struct Row {
+  static constexpr int R = 64 / L;  // rows of a wavefront
+  int i, sub;                       // lane of the row, row of the wavefront
+  int start[K];                     // first channel of the chunk
+  int lo[K], hi[K];                 // its channels that count: [lo, hi); those under hi exist; hi = 0: no chunk
+  int e[K];                         // entry
+  int d[K], rel[K], f0[K];          // components of a field, first channel within the entry, first field of the entry
+  int gate[K];                      // gate of the entry's first field
+  int blk[K], blk_lo[K], quad[K];   // exponent byte, that of the channels under lo, place of the chunk in its block
+  float m[K], rm[K];                // fields of the entry, and 1 / m
+  bool scalar[K];
+  bool any_scalar;                  // uniform
+  int n;
+  int last;                         // ds_bpermute address of the last lane of the run (K = 1)
+  int mate[3];                      // and of the lanes of the same block
+  bool ok1, ok2, ok4, ok8, ok15, ok31;
+
+  __device__ __forceinline__ void init(const SiteTab& t, int entries) {
+    const int lane = threadIdx.x & 63;
+    i = lane & (L - 1);
+    sub = lane / L;
+    n = entries;
+    any_scalar = false;
+    int seg0 = 0, seg1 = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      start[k] = lo[k] = hi[k] = rel[k] = f0[k] = gate[k] = blk[k] = blk_lo[k] = quad[k] = 0;
+      e[k] = -1;
+      d[k] = 1;
+      m[k] = 1.f;
+      scalar[k] = false;
+    }
+    for (int en = 0; en < entries; ++en) {
+      const int t0 = t.t0[en], t1 = t.t0[en + 1], ch0 = t.ch0[en], w = t.ch0[en + 1] - ch0;
+      any_scalar |= t.l[en] == 0;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int c = i + k * L;
+        if (c < t0 || c >= t1) continue;
+        const int j = c - t0, at = 8 * j;
+        int s = at, first = 0, end = 8;
+        if (RAG && at + 8 > w) {
+          if (w >= 8) {
+            s = w - 8;
+            first = at - s;
+          } else {
+            end = w;
+          }
+        }
+        start[k] = ch0 + s;
+        rel[k] = s;
+        lo[k] = first;
+        hi[k] = end;
+        e[k] = en;
+        d[k] = 2 * t.l[en] + 1;
+        f0[k] = t.f0[en];
+        gate[k] = t.gate0[en];
+        blk[k] = t.b0[en] + j / 4;
+        blk_lo[k] = t.b0[en] + (j > 0 ? j - 1 : 0) / 4;
+        quad[k] = j & 3;
+        m[k] = (float)t.mult[en];
+        scalar[k] = t.l[en] == 0;
+        if (k == 0) seg0 = t0, seg1 = t1 - 1;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) rm[k] = 1.f / m[k];
+    if (K == 1) {
+      if (hi[0] == 0) seg0 = seg1 = i;  // a lane without a chunk is a run of its own
+      const int base = lane - i;
+      last = 4 * (base + seg1);
+      ok1 = i - 1 >= seg0;
+      ok2 = i - 2 >= seg0;
+      ok4 = i - 4 >= seg0;
+      ok8 = i - 8 >= seg0;
+      ok15 = seg0 < (i & ~15);
+      ok31 = seg0 < 32;
+#pragma unroll
+      for (int b = 0; b < 3; ++b) mate[b] = 4 * (base + min(i - quad[0] + ((quad[0] + b + 1) & 3), seg1));
+    }
+  }
+
+  __device__ __forceinline__ int field(int k, int v) const {  // of channel v of the chunk, in its entry; < 1024 channels
+    return ((rel[k] + v) * (65536 / d[k] + 1)) >> 16;
+  }
+
+  // The channels of a chunk of a row that starts at p; zeros where there are none.
+  template <typename T>
+  __device__ __forceinline__ f8 load(const T* p, int k) const {
+    f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (!RAG || hi[k] == 8 || hi[k] == 0) {
+      if (hi[k]) v = load8<T>(p + start[k]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 7; ++c)
+        if (c < hi[k]) v[c] = DT<T>::to_f(p[start[k] + c]);
+    }
+    return v;
+  }
+
+  // The same of a checkpoint: row of the int8 values and of the exponent bytes.
+  __device__ __forceinline__ f8 load_packed(const int8_t* p, const uint8_t* b, int k) const {
+    f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (hi[k] == 0) return v;
+    u2 q = {0, 0};
+    if (!RAG || hi[k] == 8) {
+      q = *reinterpret_cast<const u2_any*>(p + start[k]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 7; ++c)
+        if (c < hi[k]) q[c / 4] |= (uint32_t)(uint8_t)p[start[k] + c] << (8 * (c & 3));
+    }
+    const float s = pack_scale(b[blk[k]]);
+    const float s_lo = RAG && lo[k] > 0 ? pack_scale(b[blk_lo[k]]) : s;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      v[c] = (float)(int8_t)(q[c / 4] >> (8 * (c & 3))) * (RAG && c < lo[k] ? s_lo : s);
+    if (RAG && hi[k] < 8)  // 0 * NaN
+#pragma unroll
+      for (int c = 1; c < 8; ++c)
+        if (c >= hi[k]) v[c] = 0.f;
+    return v;
+  }
+
+  template <typename T>
+  __device__ __forceinline__ void store(T* p, int k, f8 v) const {
+    if (!RAG || hi[k] == 8 || hi[k] == 0) {
+      if (hi[k]) store8(p + start[k], v);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 7; ++c)
+        if (c < hi[k]) p[start[k] + c] = DT<T>::from_f(v[c]);
+    }
+  }
+
+  __device__ __forceinline__ bool counts(int k, int c) const { return !RAG || (c >= lo[k] && c < hi[k]); }
+
+  __device__ __forceinline__ float of(f8 v, int k) const {  // sum of the chunk's channels that count
+    float s[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s[c] = counts(k, c) ? v[c] : 0.f;
+    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+  }
+  __device__ __forceinline__ float dot(f8 a, f8 b, int k) const {
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; c += 2) {
+      s0 = counts(k, c) ? fmaf(a[c], b[c], s0) : s0;
+      s1 = counts(k, c + 1) ? fmaf(a[c + 1], b[c + 1], s1) : s1;
+    }
+    return s0 + s1;
+  }
+
+  // Sums over the entry of every chunk, of one or two values a chunk.
+  template <int N>
+  __device__ __forceinline__ void sums(float (&v)[N][K]) const {
+    if constexpr (K == 1) {
+#define SSK_STEP(CTRL, ROWS, OK)                                   \
+  {                                                                \
+    float s_[N];                                                   \
+    _Pragma("unroll") for (int a = 0; a < N; ++a) s_[a] = dpp_or_0<CTRL, ROWS>(v[a][0]); \
+    _Pragma("unroll") for (int a = 0; a < N; ++a) v[a][0] += (OK) ? s_[a] : 0.f;          \
+  }
+      SSK_STEP(0x111, 0xf, ok1)
+      SSK_STEP(0x112, 0xf, ok2)
+      SSK_STEP(0x114, 0xf, ok4)
+      SSK_STEP(0x118, 0xf, ok8)
+      if constexpr (L >= 32) SSK_STEP(0x142, 0xa, ok15)  // lane 15 of the row of 16 before
+      if constexpr (L >= 64) SSK_STEP(0x143, 0xc, ok31)  // lane 31
+#undef SSK_STEP
+#pragma unroll
+      for (int a = 0; a < N; ++a) v[a][0] = read_lane(v[a][0], last);
+    } else {
+      float out[N][K] = {};
+      for (int en = 0; en < n; ++en)
+#pragma unroll
+        for (int a = 0; a < N; ++a) {
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < K; ++k) s += e[k] == en ? v[a][k] : 0.f;
+#pragma unroll
+          for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
+#pragma unroll
+          for (int k = 0; k < K; ++k) out[a][k] = e[k] == en ? s : out[a][k];
+        }
+#pragma unroll
+      for (int a = 0; a < N; ++a)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[a][k] = out[a][k];
+    }
+  }
+
+  // s / m with one correction step: exact where the quotient is a value of fp32 (a mean that equals one of its
+  // values gives a difference of exactly zero, on which a relu turns).
+  __device__ __forceinline__ float over_m(float s, int k) const {
+    const float q = s * rm[k];
+    const float r = fmaf(fmaf(-q, m[k], s), rm[k], q);
+    return fabsf(q) < 3e38f ? r : q;
+  }
+
+  // xhat in place of x; r = 1 / sqrt(v + eps).
+  __device__ __forceinline__ void norm(f8 (&x)[K], float (&r)[K], float eps) const {
+    if (any_scalar) {
+      float s[1][K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) s[0][k] = of(x[k], k);
+      sums(s);
+#pragma unroll
+      for (int k = 0; k < K; ++k) x[k] -= scalar[k] ? over_m(s[0][k], k) : 0.f;
+    }
+    float s[1][K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[0][k] = dot(x[k], x[k], k);
+    sums(s);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      r[k] = __builtin_amdgcn_rsqf(fmaf(s[0][k], rm[k], eps));
+      x[k] *= r[k];
+    }
+  }
+
+  // Gradient behind a norm in place of t = gain * dy, from xhat and r.
+  __device__ __forceinline__ void norm_back(const f8 (&xhat)[K], const float (&r)[K], f8 (&t)[K]) const {
+    float s[2][K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      s[0][k] = of(t[k], k);
+      s[1][k] = dot(t[k], xhat[k], k);
+    }
+    sums(s);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const float a = scalar[k] ? s[0][k] * rm[k] : 0.f, b = s[1][k] * rm[k];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) t[k][c] = r[k] * (t[k][c] - a - xhat[k][c] * b);
+    }
+  }
+
+  // A parameter per field as one per channel of the chunks (ones without it).
+  __device__ __forceinline__ void params(const float* p, f8 (&v)[K], int entries) const {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        v[k][c] = p && e[k] < entries && c < hi[k] ? p[f0[k] + field(k, c)] : 1.f;
+  }
+
+  // The checkpoint of a row: int8 values at q, exponent bytes at b; of the chunks of the first `entries` entries.
+  __device__ __forceinline__ void pack(const f8 (&x)[K], int8_t* q, uint8_t* b, int entries, bool on) const {
+    uint32_t amax[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      amax[k] = 0;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (counts(k, c)) amax[k] = max(amax[k], __float_as_uint(x[k][c]) & 0x7fffffffu);
+    }
+    // the chunks of a block lie in up to four neighbouring lanes
+    if constexpr (K == 1) {
+      uint32_t o[3];
+#pragma unroll
+      for (int a = 0; a < 3; ++a) o[a] = (uint32_t)__builtin_amdgcn_ds_bpermute(mate[a], (int)amax[0]);
+      amax[0] = max(max(amax[0], o[0]), max(o[1], o[2]));
+    } else {  // lane i of chunk row k is chunk i + 64 k of the row
+      uint32_t all[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) all[k] = amax[k];
+#pragma unroll
+      for (int s = -3; s <= 3; ++s) {
+        if (s == 0) continue;
+        uint32_t far[K];
+        int blk_far[K];
+        const int to = (i + s) & 63;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          far[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * to, (int)amax[k]);
+          blk_far[k] = __builtin_amdgcn_ds_bpermute(4 * to, hi[k] ? blk[k] : -1);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const int kk = k + (i + s < 0 ? -1 : i + s > 63 ? 1 : 0);
+#pragma unroll
+          for (int o = 0; o < K; ++o)
+            if (o == kk && blk_far[o] == blk[k]) all[k] = max(all[k], far[o]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) amax[k] = all[k];
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!on || hi[k] == 0 || e[k] >= entries) continue;
+      const int byte = pack_byte(amax[k]);
+      const float inv = pack_inverse(byte);
+      // 1.5 2^23 + v has v, rounded to nearest even, in its low bits
+      uint32_t w[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) w[c] = byte == 255 ? 0u : __float_as_uint(fmaf(x[k][c], inv, 12582912.f));
+      if (!RAG || (lo[k] == 0 && hi[k] == 8)) {
+        u2 p;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          const uint32_t l16 = __builtin_amdgcn_perm(w[4 * a + 1], w[4 * a], 0x0c0c0400u);
+          const uint32_t h16 = __builtin_amdgcn_perm(w[4 * a + 3], w[4 * a + 2], 0x04000c0cu);
+          p[a] = l16 | h16;
+        }
+        *reinterpret_cast<u2_any*>(q + start[k]) = p;
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (counts(k, c)) q[start[k] + c] = (int8_t)w[c];
+      }
+      if (quad[k] == 0) b[blk[k]] = (uint8_t)byte;
+    }
+  }
+};
+
+// Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order, to out[channels];
+// lds holds one row of floats per row that the workgroup takes at a time.  All threads call it.
+template <int L, int K, bool RAG>
+__device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc)[K], int channels, float* lds,
+                                         float* out) {
+  constexpr int ROWS = kSiteNT / L;
+  __syncthreads();
+  float* mine = lds + ((threadIdx.x >> 6) * (64 / L) + w.sub) * channels;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      if (w.hi[k] > 0 && w.counts(k, c) && w.start[k] + c < channels) mine[w.start[k] + c] = acc[k][c];
+  __syncthreads();
+  for (int c = threadIdx.x; c < channels; c += kSiteNT) {
+    float s = 0.f;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) s += lds[r * channels + c];
+    out[c] = s;
+  }
+}
+
+// GO_(L, K, RAG) for a table.
+#define SSK_SITE_DISPATCH(t_, GO_)                                   \
+  do {                                                               \
+    const int chunks_ = (t_).t0[(t_).n];                             \
+    if ((t_).ragged) {                                               \
+      if (chunks_ <= 16) GO_(16, 1, true);                           \
+      if (chunks_ <= 32) GO_(32, 1, true);                           \
+      if (chunks_ <= 64) GO_(64, 1, true);                           \
+      GO_(64, 3, true);                                              \
+    }                                                                \
+    if (chunks_ <= 16) GO_(16, 1, false);                            \
+    if (chunks_ <= 32) GO_(32, 1, false);                            \
+    if (chunks_ <= 64) GO_(64, 1, false);                            \
+    GO_(64, 3, false);                                               \
+  } while (0)
+
+}  // namespace ssconv
