@@ -29,6 +29,9 @@ int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t) {
     t->f0[e] = (int)fi;
     t->b0[e] = (int)b;
     t->t0[e] = (int)tc;
+    t->inv[e] = 65536 / (2 * t->l[e] + 1) + 1;
+    t->m[e] = (float)t->mult[e];
+    t->rm[e] = 1.f / t->m[e];
     ch += w;
     fi += t->mult[e];
     b += (w + kPackBlock - 1) / kPackBlock;
@@ -42,26 +45,36 @@ int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t) {
 
 namespace {
 
-// out[f] = sum of the workgroups' partial sums over the components of field f, in fp64 and a fixed order: one workgroup
-// a field, since the partials (up to 1024 rows of them) lie in the L2s.
+struct ReduceArgs {
+  float* out[3];
+  int at[3];     // first channel of each in a row of partials
+  int f_end[3];  // workgroups up to this one are its fields
+};
+
+// Gradients of up to three parameters: out[f] = sum of the workgroups' partial sums over the components of field f, in
+// fp64 and a fixed order.  One workgroup a field, since the partials (up to 2048 rows of them) lie in the L2s.
 __global__ __launch_bounds__(kSiteNT) void site_reduce(SiteTab t, const float* __restrict__ part, int blocks, int stride,
-                                                       float* __restrict__ out) {
+                                                       ReduceArgs a) {
   __shared__ double wave[kSiteNT / 64];
-  const int f = blockIdx.x;
+  const int p = blockIdx.x < a.f_end[0] ? 0 : blockIdx.x < a.f_end[1] ? 1 : 2;
+  const int f = blockIdx.x - (p ? a.f_end[p - 1] : 0);
   int e = 0;
   while (f >= t.f0[e + 1]) ++e;
-  const int d = 2 * t.l[e] + 1, c0 = t.ch0[e] + (f - t.f0[e]) * d;
+  const int d = 2 * t.l[e] + 1, c0 = a.at[p] + t.ch0[e] + (f - t.f0[e]) * d;
   double s = 0.0;
   for (int b = threadIdx.x; b < blocks; b += kSiteNT)
     for (int i = 0; i < d; ++i) s += (double)part[(int64_t)b * stride + c0 + i];
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) out[f] = (float)(((wave[0] + wave[1]) + wave[2]) + wave[3]);
+  if (threadIdx.x == 0) a.out[p][f] = (float)(((wave[0] + wave[1]) + wave[2]) + wave[3]);
 }
 
-int reduce_fields(const SiteTab& t, const float* part, unsigned blocks, int stride, float* out, hipStream_t st) {
-  site_reduce<<<t.f0[t.n], kSiteNT, 0, st>>>(t, part, (int)blocks, stride, out);
+// t: the entries of the longest list among the parameters; the others are its beginning.
+int reduce_fields(const SiteTab& t, const float* part, unsigned blocks, int stride, const ReduceArgs& a,
+                  hipStream_t st) {
+  if (a.f_end[2] == 0) return SSCONV_OK;
+  site_reduce<<<a.f_end[2], kSiteNT, 0, st>>>(t, part, (int)blocks, stride, a);
   SSC_HIP(hipGetLastError());
   return SSCONV_OK;
 }
@@ -78,7 +91,11 @@ int check_workspace(const void* ws, size_t bytes, size_t need) {
   return SSCONV_OK;
 }
 
-size_t ws_bytes_of(const SiteTab& t, int64_t n, int floats) { return (size_t)site_blocks(t, n, kBwdPerCu) * floats * 4; }
+// A row of partial sums of every workgroup.
+size_t norm_ws_bytes(const SiteTab& t, int64_t n) { return (size_t)site_blocks(t, n, norm_bwd_per_cu) * t.C * 4; }
+size_t tail_ws_bytes(const SiteTab& t, int64_t n) {
+  return (size_t)site_blocks(t, n, tail_bwd_per_cu) * (t.ch0[t.n] + 2 * t.C) * 4;
+}
 
 }  // namespace
 
@@ -139,7 +156,7 @@ extern "C" int ssconv_site_norm_forward(const ssconv_fields* fields, const sscon
 extern "C" size_t ssconv_site_norm_workspace_size(const ssconv_fields* fields, int64_t n) {
   SiteTab t;
   if (n < 0 || make_sitetab(fields, false, &t) != SSCONV_OK) return 0;
-  return ws_bytes_of(t, n, t.C);
+  return norm_ws_bytes(t, n);
 }
 
 extern "C" int ssconv_site_norm_backward(const ssconv_fields* fields, const ssconv_rows* x, const void* dy,
@@ -150,7 +167,7 @@ extern "C" int ssconv_site_norm_backward(const ssconv_fields* fields, const ssco
   SSC_TRY(check_site(fields, false, dtype, n, &t));
   SSC_TRY(check_site_eps(eps));
   if (n > 0 && (!x || !x->data || !dy || !dx)) return fail(SSCONV_E_INVALID, "NULL feature buffer");
-  if (dgain && n > 0) SSC_TRY(check_workspace(workspace, ws_bytes, ws_bytes_of(t, n, t.C)));
+  if (dgain && n > 0) SSC_TRY(check_workspace(workspace, ws_bytes, norm_ws_bytes(t, n)));
   float* part = dgain && n > 0 ? (float*)workspace : nullptr;
   if (n > 0) {
     NormArgs a{};
@@ -164,7 +181,8 @@ extern "C" int ssconv_site_norm_backward(const ssconv_fields* fields, const ssco
     a.part = part;
     SSC_TRY(launch_norm_bwd(t, dtype, a, stream));
   }
-  return dgain ? reduce_fields(t, part, site_blocks(t, n, kBwdPerCu), t.C, dgain, stream) : SSCONV_OK;
+  const int F = dgain ? t.f0[t.n] : 0;
+  return reduce_fields(t, part, site_blocks(t, n, norm_bwd_per_cu), t.C, ReduceArgs{{dgain}, {0}, {F, F, F}}, stream);
 }
 
 extern "C" int ssconv_residual_forward(const ssconv_fields* fields, const void* y, const void* h, ssconv_dtype dtype,
@@ -199,7 +217,7 @@ extern "C" int ssconv_residual_forward(const ssconv_fields* fields, const void* 
 extern "C" size_t ssconv_residual_workspace_size(const ssconv_fields* fields, int64_t n) {
   SiteTab t;
   if (n < 0 || make_sitetab(fields, true, &t) != SSCONV_OK) return 0;
-  return ws_bytes_of(t, n, t.ch0[t.n] + 2 * t.C);
+  return tail_ws_bytes(t, n);
 }
 
 extern "C" int ssconv_residual_backward(const ssconv_fields* fields, const ssconv_rows* y, const ssconv_rows* h_out,
@@ -207,9 +225,8 @@ extern "C" int ssconv_residual_backward(const ssconv_fields* fields, const sscon
                                         const float* gain_post, const float* scale, const float* gain_next, void* dy,
                                         void* dh_in, float* dgain_post, float* dscale, float* dgain_next,
                                         void* workspace, size_t ws_bytes, hipStream_t stream) {
-  SiteTab ty, th;
+  SiteTab ty;
   SSC_TRY(check_site(fields, true, dtype, n, &ty));
-  SSC_TRY(make_sitetab(fields, false, &th));
   SSC_TRY(check_site_eps(eps));
   if (n > 0 && (!y || !y->data || !dh || !dy || !dh_in)) return fail(SSCONV_E_INVALID, "NULL feature buffer");
   if (n > 0 && dx && (!h_out || !h_out->data)) return fail(SSCONV_E_INVALID, "dx needs h_out");
@@ -217,7 +234,7 @@ extern "C" int ssconv_residual_backward(const ssconv_fields* fields, const sscon
   const int S = ty.ch0[ty.n], C = ty.C, stride = S + 2 * C;
   float* part = nullptr;
   if (n > 0 && (dgain_post || dscale || dgain_next)) {
-    SSC_TRY(check_workspace(workspace, ws_bytes, ws_bytes_of(ty, n, stride)));
+    SSC_TRY(check_workspace(workspace, ws_bytes, tail_ws_bytes(ty, n)));
     part = (float*)workspace;
   }
   if (n > 0) {
@@ -236,9 +253,10 @@ extern "C" int ssconv_residual_backward(const ssconv_fields* fields, const sscon
     a.part = part;
     SSC_TRY(launch_tail_bwd(ty, dtype, a, stream));
   }
-  const unsigned nb = site_blocks(ty, n, kBwdPerCu);
-  if (dgain_post) SSC_TRY(reduce_fields(ty, part, nb, stride, dgain_post, stream));
-  if (dscale) SSC_TRY(reduce_fields(th, part ? part + S : nullptr, nb, stride, dscale, stream));
-  if (dgain_next) SSC_TRY(reduce_fields(th, part ? part + S + C : nullptr, nb, stride, dgain_next, stream));
-  return SSCONV_OK;
+  const int F = ty.f0[ty.n_regular], FS = ty.f0[ty.n];
+  ReduceArgs r{{dgain_post, dscale, dgain_next}, {0, S, S + C}, {}};
+  r.f_end[0] = dgain_post ? FS : 0;
+  r.f_end[1] = r.f_end[0] + (dscale ? F : 0);
+  r.f_end[2] = r.f_end[1] + (dgain_next ? F : 0);
+  return reduce_fields(ty, part, site_blocks(ty, n, tail_bwd_per_cu), stride, r, stream);
 }

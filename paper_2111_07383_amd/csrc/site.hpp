@@ -23,6 +23,8 @@ struct SiteTab {
   int b0[SSCONV_MAX_ENTRIES + 1];   // first checkpoint block, b0[n] = blocks of a row
   int t0[SSCONV_MAX_ENTRIES + 1];   // first chunk, t0[n] = chunks of a row
   int gate0[SSCONV_MAX_ENTRIES];    // gate of the first field of each entry (entries of order > 0)
+  int inv[SSCONV_MAX_ENTRIES];      // 65536 / components + 1: channel -> field without a division
+  float m[SSCONV_MAX_ENTRIES], rm[SSCONV_MAX_ENTRIES];  // fields, and 1 / fields
   int C, G;                         // channels without the gates, gates
   int n_regular;                    // entries without the gates'
   int ragged;                       // some entry is not a multiple of 8 channels
@@ -31,21 +33,29 @@ struct SiteTab {
 // gated: the gates of the fields of order > 0 as one more entry.
 int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t);
 
-// Lanes per row and chunks per lane: the fewest lanes that hold a row, one chunk each, or 64 lanes with three.
+// Lanes per row: the fewest that hold a row with one chunk each, or 64 with three.
 inline int site_lanes(const SiteTab& t) {
   const int c = t.t0[t.n];
   return c <= 16 ? 16 : c <= 32 ? 32 : 64;
 }
+inline bool site_wide(const SiteTab& t) { return t.t0[t.n] > 64; }
+// Floats of LDS per row of the residual tail: the row, and 8 that a chunk moved off it may read.
+inline int site_lds_row(const SiteTab& t) { return (t.ch0[t.n] + 8 + 7) / 8 * 8; }
 // Rows that a workgroup takes at a time.
 inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 
-// Workgroups of a call: all rows at once where they are few, else as many as stay on the chip, which then loop.
-inline unsigned site_blocks(const SiteTab& t, int64_t n, int per_cu) {
+// Workgroups of a compute unit at a time, by a kernel's registers (their launch bounds); a workgroup is one wavefront
+// per SIMD.  All loop over the rows, so a grid of more would run in rounds of which the last is part empty (backward of
+// a 208-channel tail: 1024 workgroups of which 768 fit 235 us).
+constexpr int norm_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 4 : rag ? 5 : 8; }
+constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag || L == 64 ? 5 : 8; }
+constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag ? 4 : 6; }
+constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : L == 64 ? 3 : 4; }
+inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
   const int64_t rows = site_rows(t);
-  return (unsigned)std::min<int64_t>((n + rows - 1) / rows, 256 * per_cu);
+  return (unsigned)std::min<int64_t>((n + rows - 1) / rows,
+                                     256 * per_cu(site_lanes(t), site_wide(t) ? 3 : 1, t.ragged != 0));
 }
-constexpr int kFwdPerCu = 8;
-constexpr int kBwdPerCu = 4;  // each leaves a row of partial sums of the parameters' gradients
 
 struct NormArgs {
   ssconv_rows x;

@@ -7,7 +7,7 @@ namespace ssconv {
 namespace {
 
 template <typename T, int L, int K, bool RAG>
-__global__ __launch_bounds__(kSiteNT) void norm_fwd_kernel(SiteTab t, NormArgs a) {
+__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void norm_fwd_kernel(SiteTab t, NormArgs a) {
   using R = Row<L, K, RAG>;
   R w;
   w.init(t, t.n);
@@ -15,25 +15,23 @@ __global__ __launch_bounds__(kSiteNT) void norm_fwd_kernel(SiteTab t, NormArgs a
   f8 g[K];
   w.params(a.gain, g, t.n);
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
-  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < a.n; r0 += step) {
-    const bool on = r0 + w.sub < a.n;
-    const int64_t row = on ? r0 + w.sub : a.n - 1;
+  for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
+    const bool on = w.sub < a.n - r0;
+    const int row = w.row_of(a.n - r0);
     f8 x[K];
     float r[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-      x[k] = a.x.exps ? w.load_packed((const int8_t*)a.x.data + row * C, a.x.exps + row * B, k)
-                      : w.template load<T>((const T*)a.x.data + row * C, k);
-    if (a.q) w.pack(x, a.q + row * C, a.exps + row * B, t.n, on);
+    for (int k = 0; k < K; ++k) x[k] = w.template load_rows<T>(a.x, r0, row, C, B, k, w.start[k], w.blk[k]);
+    if (a.q) w.pack(x, a.q + r0 * C, a.exps + r0 * B, row, C, B, t.n, on);
     w.norm(x, r, a.eps);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (on) w.template store<T>((T*)a.out + row * C, k, x[k] * g[k]);
+      if (on) w.template store<T>((T*)a.out + r0 * C, row, C, k, x[k] * g[k]);
   }
 }
 
 template <typename T, int L, int K, bool RAG>
-__global__ __launch_bounds__(kSiteNT) void norm_bwd_kernel(SiteTab t, NormArgs a) {
+__global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_kernel(SiteTab t, NormArgs a) {
   extern __shared__ float lds[];
   using R = Row<L, K, RAG>;
   R w;
@@ -44,18 +42,17 @@ __global__ __launch_bounds__(kSiteNT) void norm_bwd_kernel(SiteTab t, NormArgs a
 #pragma unroll
   for (int k = 0; k < K; ++k) acc[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
-  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < a.n; r0 += step) {
-    const bool on = r0 + w.sub < a.n;
-    const int64_t row = on ? r0 + w.sub : a.n - 1;
+  for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
+    const bool on = w.sub < a.n - r0;
+    const int row = w.row_of(a.n - r0);
     f8 x[K], d[K], res[K];
     float r[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k] = a.x.exps ? w.load_packed((const int8_t*)a.x.data + row * C, a.x.exps + row * B, k)
-                      : w.template load<T>((const T*)a.x.data + row * C, k);
-      d[k] = w.template load<T>((const T*)a.dy + row * C, k);
+      x[k] = w.template load_rows<T>(a.x, r0, row, C, B, k, w.start[k], w.blk[k]);
+      d[k] = w.template load<T>((const T*)a.dy + r0 * C, row, C, k, w.start[k]);
       res[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (a.dres) res[k] = w.template load<T>((const T*)a.dres + row * C, k);
+      if (a.dres) res[k] = w.template load<T>((const T*)a.dres + r0 * C, row, C, k, w.start[k]);
     }
     w.norm(x, r, a.eps);
 #pragma unroll
@@ -66,48 +63,48 @@ __global__ __launch_bounds__(kSiteNT) void norm_bwd_kernel(SiteTab t, NormArgs a
     w.norm_back(x, r, d);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (on) w.template store<T>((T*)a.out + row * C, k, d[k] + res[k]);
+      if (on) w.template store<T>((T*)a.out + r0 * C, row, C, k, d[k] + res[k]);
   }
   if (a.part) sum_rows<L, K, RAG>(w, acc, C, lds, a.part + (int64_t)blockIdx.x * C);
 }
 
 template <typename T, int L, int K, bool RAG>
-__global__ __launch_bounds__(kSiteNT) void pack_kernel(SiteTab t, const T* x, int64_t n, int8_t* q, uint8_t* exps) {
+__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kernel(SiteTab t, const T* x, int64_t n, int8_t* q, uint8_t* exps) {
   using R = Row<L, K, RAG>;
   R w;
   w.init(t, t.n);
   const int C = t.ch0[t.n], B = t.b0[t.n];
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
-  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < n; r0 += step) {
-    const bool on = r0 + w.sub < n;
-    const int64_t row = on ? r0 + w.sub : n - 1;
+  for (int64_t r0 = first_row<R::R>(); r0 < n; r0 += step) {
+    const bool on = w.sub < n - r0;
+    const int row = w.row_of(n - r0);
     f8 v[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = w.template load<T>(x + row * C, k);
-    w.pack(v, q + row * C, exps + row * B, t.n, on);
+    for (int k = 0; k < K; ++k) v[k] = w.template load<T>(x + r0 * C, row, C, k, w.start[k]);
+    w.pack(v, q + r0 * C, exps + r0 * B, row, C, B, t.n, on);
   }
 }
 
 template <typename T, int L, int K, bool RAG>
-__global__ __launch_bounds__(kSiteNT) void unpack_kernel(SiteTab t, const int8_t* q, const uint8_t* exps, int64_t n,
+__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void unpack_kernel(SiteTab t, const int8_t* q, const uint8_t* exps, int64_t n,
                                                          T* x) {
   using R = Row<L, K, RAG>;
   R w;
   w.init(t, t.n);
   const int C = t.ch0[t.n], B = t.b0[t.n];
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
-  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < n; r0 += step) {
-    const int64_t row = r0 + w.sub;
-    if (row < n)
+  for (int64_t r0 = first_row<R::R>(); r0 < n; r0 += step) {
+    if (w.sub < n - r0)
 #pragma unroll
-      for (int k = 0; k < K; ++k) w.template store<T>(x + row * C, k, w.load_packed(q + row * C, exps + row * B, k));
+      for (int k = 0; k < K; ++k)
+        w.template store<T>(x + r0 * C, w.sub, C, k, w.load_packed(q + r0 * C, exps + r0 * B, w.sub, C, B, k, w.start[k], w.blk[k]));
   }
 }
 
 }  // namespace
 
 int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st) {
-  const unsigned nb = site_blocks(t, a.n, kFwdPerCu);
+  const unsigned nb = site_blocks(t, a.n, norm_fwd_per_cu);
   auto go = [&](auto kernel) {
     kernel<<<nb, kSiteNT, 0, st>>>(t, a);
     SSC_HIP(hipGetLastError());
@@ -120,7 +117,7 @@ int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStr
 }
 
 int launch_norm_bwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st) {
-  const unsigned nb = site_blocks(t, a.n, kBwdPerCu);
+  const unsigned nb = site_blocks(t, a.n, norm_bwd_per_cu);
   const size_t lds = a.part ? (size_t)site_rows(t) * t.ch0[t.n] * 4 : 0;
   auto go = [&](auto kernel) {
     kernel<<<nb, kSiteNT, lds, st>>>(t, a);
@@ -135,7 +132,7 @@ int launch_norm_bwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStr
 
 int launch_pack(const SiteTab& t, ssconv_dtype dt, const void* x, int64_t n, int8_t* q, uint8_t* exps,
                 hipStream_t st) {
-  const unsigned nb = site_blocks(t, n, kFwdPerCu);
+  const unsigned nb = site_blocks(t, n, norm_fwd_per_cu);
   auto go = [&](auto kernel, auto* p) {
     kernel<<<nb, kSiteNT, 0, st>>>(t, p, n, q, exps);
     SSC_HIP(hipGetLastError());
@@ -150,7 +147,7 @@ int launch_pack(const SiteTab& t, ssconv_dtype dt, const void* x, int64_t n, int
 
 int launch_unpack(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, void* x,
                   hipStream_t st) {
-  const unsigned nb = site_blocks(t, n, kFwdPerCu);
+  const unsigned nb = site_blocks(t, n, norm_fwd_per_cu);
   auto go = [&](auto kernel, auto* p) {
     kernel<<<nb, kSiteNT, 0, st>>>(t, q, exps, n, p);
     SSC_HIP(hipGetLastError());

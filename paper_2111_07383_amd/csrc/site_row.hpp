@@ -44,9 +44,9 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 __device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float dpp_or_0(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, true));
+template <int CTRL>
+__device__ __forceinline__ float dpp_or_0(float v) {  // the value of another lane, 0 where there is none
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
 __device__ __forceinline__ float read_lane(float v, int addr) {
@@ -84,15 +84,21 @@ __device__ __forceinline__ void store8(uint16_t* p, f8 v) {
   *reinterpret_cast<u4_any*>(p) = __builtin_bit_cast(u4, __builtin_convertvector(v, bf8));
 }
 
+// First row of a wavefront that takes ROWS at a time, in scalar registers.
+template <int ROWS>
+__device__ __forceinline__ int64_t first_row() {
+  return ((int64_t)blockIdx.x * (kSiteNT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * ROWS;
+}
+
 template <int L, int K, bool RAG>
 struct Row {
-  static constexpr int R = 64 / L;  // rows of a wavefront
+  static constexpr int R = 64 / L;            // rows of a wavefront
+  static constexpr int Q = K == 1 ? 2 : 4;    // gates of a lane: a row of 8 L K channels has at most 2 L K of them
   int i, sub;                       // lane of the row, row of the wavefront
   int start[K];                     // first channel of the chunk
   int lo[K], hi[K];                 // its channels that count: [lo, hi); those under hi exist; hi = 0: no chunk
   int e[K];                         // entry
-  int d[K], rel[K], f0[K];          // components of a field, first channel within the entry, first field of the entry
-  int gate[K];                      // gate of the entry's first field
+  int rel[K], f0[K], inv[K];        // first channel within the entry, first field of the entry, 65536 / components + 1
   int blk[K], blk_lo[K], quad[K];   // exponent byte, that of the channels under lo, place of the chunk in its block
   float m[K], rm[K];                // fields of the entry, and 1 / m
   bool scalar[K];
@@ -100,7 +106,7 @@ struct Row {
   int n;
   int last;                         // ds_bpermute address of the last lane of the run (K = 1)
   int mate[3];                      // and of the lanes of the same block
-  bool ok1, ok2, ok4, ok8, ok15, ok31;
+  float m1, m2, m4, m8, m15, m31;   // 1 where the lane that many places before belongs to the run
 
   __device__ __forceinline__ void init(const SiteTab& t, int entries) {
     const int lane = threadIdx.x & 63;
@@ -108,100 +114,104 @@ struct Row {
     sub = lane / L;
     n = entries;
     any_scalar = false;
-    int seg0 = 0, seg1 = 0;
+    int seg0 = i, seg1 = i;  // a lane without a chunk is a run of its own
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      start[k] = lo[k] = hi[k] = rel[k] = f0[k] = gate[k] = blk[k] = blk_lo[k] = quad[k] = 0;
+      start[k] = lo[k] = hi[k] = rel[k] = f0[k] = blk[k] = blk_lo[k] = quad[k] = 0;
       e[k] = -1;
-      d[k] = 1;
-      m[k] = 1.f;
+      inv[k] = 65537;
+      m[k] = rm[k] = 1.f;
       scalar[k] = false;
     }
-    for (int en = 0; en < entries; ++en) {
+#pragma unroll
+    for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {  // those past the last hold no chunk
       const int t0 = t.t0[en], t1 = t.t0[en + 1], ch0 = t.ch0[en], w = t.ch0[en + 1] - ch0;
-      any_scalar |= t.l[en] == 0;
+      any_scalar |= en < entries && t.l[en] == 0;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int c = i + k * L;
-        if (c < t0 || c >= t1) continue;
-        const int j = c - t0, at = 8 * j;
+        const int c = i + k * L, j = c - t0, at = 8 * j;
+        const bool in = c >= t0 && c < t1;
         int s = at, first = 0, end = 8;
-        if (RAG && at + 8 > w) {
-          if (w >= 8) {
-            s = w - 8;
-            first = at - s;
-          } else {
-            end = w;
-          }
+        if (RAG) {
+          const bool over = at + 8 > w;
+          s = over ? max(w - 8, 0) : at;
+          first = at - s;
+          end = min(w, 8);
         }
-        start[k] = ch0 + s;
-        rel[k] = s;
-        lo[k] = first;
-        hi[k] = end;
-        e[k] = en;
-        d[k] = 2 * t.l[en] + 1;
-        f0[k] = t.f0[en];
-        gate[k] = t.gate0[en];
-        blk[k] = t.b0[en] + j / 4;
-        blk_lo[k] = t.b0[en] + (j > 0 ? j - 1 : 0) / 4;
-        quad[k] = j & 3;
-        m[k] = (float)t.mult[en];
-        scalar[k] = t.l[en] == 0;
-        if (k == 0) seg0 = t0, seg1 = t1 - 1;
+        start[k] = in ? ch0 + s : start[k];
+        rel[k] = in ? s : rel[k];
+        lo[k] = in ? first : lo[k];
+        hi[k] = in ? end : hi[k];
+        e[k] = in ? en : e[k];
+        inv[k] = in ? t.inv[en] : inv[k];
+        f0[k] = in ? t.f0[en] : f0[k];
+        blk[k] = in ? t.b0[en] + j / 4 : blk[k];
+        blk_lo[k] = in ? t.b0[en] + max(j - 1, 0) / 4 : blk_lo[k];
+        quad[k] = in ? j & 3 : quad[k];
+        m[k] = in ? t.m[en] : m[k];
+        rm[k] = in ? t.rm[en] : rm[k];
+        scalar[k] = in ? t.l[en] == 0 : scalar[k];
+        if (k == 0) seg0 = in ? t0 : seg0, seg1 = in ? t1 - 1 : seg1;
       }
     }
-#pragma unroll
-    for (int k = 0; k < K; ++k) rm[k] = 1.f / m[k];
     if (K == 1) {
-      if (hi[0] == 0) seg0 = seg1 = i;  // a lane without a chunk is a run of its own
       const int base = lane - i;
       last = 4 * (base + seg1);
-      ok1 = i - 1 >= seg0;
-      ok2 = i - 2 >= seg0;
-      ok4 = i - 4 >= seg0;
-      ok8 = i - 8 >= seg0;
-      ok15 = seg0 < (i & ~15);
-      ok31 = seg0 < 32;
+      m1 = i - 1 >= seg0 ? 1.f : 0.f;
+      m2 = i - 2 >= seg0 ? 1.f : 0.f;
+      m4 = i - 4 >= seg0 ? 1.f : 0.f;
+      m8 = i - 8 >= seg0 ? 1.f : 0.f;
+      m15 = (i & 16) && seg0 < (i & ~15) ? 1.f : 0.f;
+      m31 = i >= 32 && seg0 < 32 ? 1.f : 0.f;
 #pragma unroll
       for (int b = 0; b < 3; ++b) mate[b] = 4 * (base + min(i - quad[0] + ((quad[0] + b + 1) & 3), seg1));
     }
   }
 
   __device__ __forceinline__ int field(int k, int v) const {  // of channel v of the chunk, in its entry; < 1024 channels
-    return ((rel[k] + v) * (65536 / d[k] + 1)) >> 16;
+    return ((rel[k] + v) * inv[k]) >> 16;
   }
 
-  // The channels of a chunk of a row that starts at p; zeros where there are none.
+  // Every matrix is addressed from the wavefront's first row (scalar registers) by 32-bit offsets of the lanes.  Rows
+  // past the last are read at the last.
+  __device__ __forceinline__ int row_of(int64_t left) const { return min(sub, (int)min(left, (int64_t)R) - 1); }
+
+  // The channels of a chunk, of row r of a matrix of C channels, from channel s on (start[k], or 0 where the chunk lies
+  // past a matrix without the gates).  Without ragged entries a lane with no chunk there reads the row's first channels,
+  // which nothing uses; else it has zeros.
   template <typename T>
-  __device__ __forceinline__ f8 load(const T* p, int k) const {
+  __device__ __forceinline__ f8 load(const void* p, int r, int C, int k, int s) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (!RAG || hi[k] == 8 || hi[k] == 0) {
-      if (hi[k]) v = load8<T>(p + start[k]);
+    const T* q = reinterpret_cast<const T*>((const char*)p + (__umul24(r, C) + s) * (uint32_t)sizeof(T));
+    if (!RAG || hi[k] == 8) {
+      v = load8<T>(q);
     } else {
 #pragma unroll
       for (int c = 0; c < 7; ++c)
-        if (c < hi[k]) v[c] = DT<T>::to_f(p[start[k] + c]);
+        if (c < hi[k]) v[c] = DT<T>::to_f(q[c]);
     }
     return v;
   }
 
-  // The same of a checkpoint: row of the int8 values and of the exponent bytes.
-  __device__ __forceinline__ f8 load_packed(const int8_t* p, const uint8_t* b, int k) const {
+  // The same of a checkpoint of C channels and B blocks: the int8 values and the exponent bytes.
+  __device__ __forceinline__ f8 load_packed(const void* p, const uint8_t* b, int r, int C, int B, int k, int s,
+                                            int bl) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (hi[k] == 0) return v;
+    if (RAG && hi[k] == 0) return v;
+    const int8_t* at = (const int8_t*)p + (uint32_t)(__umul24(r, C) + s);
     u2 q = {0, 0};
     if (!RAG || hi[k] == 8) {
-      q = *reinterpret_cast<const u2_any*>(p + start[k]);
+      q = *reinterpret_cast<const u2_any*>(at);
     } else {
 #pragma unroll
       for (int c = 0; c < 7; ++c)
-        if (c < hi[k]) q[c / 4] |= (uint32_t)(uint8_t)p[start[k] + c] << (8 * (c & 3));
+        if (c < hi[k]) q[c / 4] |= (uint32_t)(uint8_t)at[c] << (8 * (c & 3));
     }
-    const float s = pack_scale(b[blk[k]]);
-    const float s_lo = RAG && lo[k] > 0 ? pack_scale(b[blk_lo[k]]) : s;
+    const float x = pack_scale(b[(uint32_t)(__umul24(r, B) + bl)]);
+    const float x_lo = RAG && lo[k] > 0 ? pack_scale(b[(uint32_t)(__umul24(r, B) + blk_lo[k])]) : x;
 #pragma unroll
     for (int c = 0; c < 8; ++c)
-      v[c] = (float)(int8_t)(q[c / 4] >> (8 * (c & 3))) * (RAG && c < lo[k] ? s_lo : s);
+      v[c] = (float)(int8_t)(q[c / 4] >> (8 * (c & 3))) * (RAG && c < lo[k] ? x_lo : x);
     if (RAG && hi[k] < 8)  // 0 * NaN
 #pragma unroll
       for (int c = 1; c < 8; ++c)
@@ -209,14 +219,23 @@ struct Row {
     return v;
   }
 
+  // Rows, or a checkpoint of them, from row r0 on.
   template <typename T>
-  __device__ __forceinline__ void store(T* p, int k, f8 v) const {
-    if (!RAG || hi[k] == 8 || hi[k] == 0) {
-      if (hi[k]) store8(p + start[k], v);
+  __device__ __forceinline__ f8 load_rows(const ssconv_rows& x, int64_t r0, int r, int C, int B, int k, int s,
+                                          int bl) const {
+    if (x.exps) return load_packed((const int8_t*)x.data + r0 * C, x.exps + r0 * B, r, C, B, k, s, bl);
+    return load<T>((const T*)x.data + r0 * C, r, C, k, s);
+  }
+
+  template <typename T>
+  __device__ __forceinline__ void store(void* p, int r, int C, int k, f8 v) const {
+    T* q = reinterpret_cast<T*>((char*)p + (__umul24(r, C) + start[k]) * (uint32_t)sizeof(T));
+    if (!RAG || hi[k] == 8) {
+      if (hi[k]) store8(q, v);
     } else {
 #pragma unroll
       for (int c = 0; c < 7; ++c)
-        if (c < hi[k]) p[start[k] + c] = DT<T>::from_f(v[c]);
+        if (c < hi[k]) q[c] = DT<T>::from_f(v[c]);
     }
   }
 
@@ -238,25 +257,66 @@ struct Row {
     return s0 + s1;
   }
 
-  // Sums over the entry of every chunk, of one or two values a chunk.
+  // Sums over the entry of every chunk, of one or two values a chunk.  A step of the prefix sum is one instruction: the
+  // value of the lane before, times 1 or 0 by whether it belongs to the run.  0 times an infinity or a NaN of another
+  // entry would not be 0, so sums that are not finite are taken again with selections (the branch is uniform).  A lane
+  // read by DPP has to be written two wait states before, hence the s_nop.
   template <int N>
   __device__ __forceinline__ void sums(float (&v)[N][K]) const {
     if constexpr (K == 1) {
-#define SSK_STEP(CTRL, ROWS, OK)                                   \
-  {                                                                \
-    float s_[N];                                                   \
-    _Pragma("unroll") for (int a = 0; a < N; ++a) s_[a] = dpp_or_0<CTRL, ROWS>(v[a][0]); \
-    _Pragma("unroll") for (int a = 0; a < N; ++a) v[a][0] += (OK) ? s_[a] : 0.f;          \
-  }
-      SSK_STEP(0x111, 0xf, ok1)
-      SSK_STEP(0x112, 0xf, ok2)
-      SSK_STEP(0x114, 0xf, ok4)
-      SSK_STEP(0x118, 0xf, ok8)
-      if constexpr (L >= 32) SSK_STEP(0x142, 0xa, ok15)  // lane 15 of the row of 16 before
-      if constexpr (L >= 64) SSK_STEP(0x143, 0xc, ok31)  // lane 31
-#undef SSK_STEP
+      float s[N];
+      bool fine = true;
 #pragma unroll
-      for (int a = 0; a < N; ++a) v[a][0] = read_lane(v[a][0], last);
+      for (int a = 0; a < N; ++a) s[a] = v[a][0];
+      if constexpr (N == 1) {
+#define SSK_STEP(CTRL) "s_nop 1\n\tv_fmac_f32_dpp %0, %0, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
+        if constexpr (L == 16)
+          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
+              : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
+        if constexpr (L == 32)  // row_bcast:15: lane 15 of the 16 before
+          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
+              SSK_STEP("5 row_bcast:15") : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15));
+        if constexpr (L == 64)  // row_bcast:31: lane 31
+          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
+              SSK_STEP("5 row_bcast:15") SSK_STEP("6 row_bcast:31")
+              : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15), "v"(m31));
+#undef SSK_STEP
+      } else {
+#define SSK_STEP(CTRL)                                                                  \
+  "s_nop 1\n\tv_fmac_f32_dpp %0, %0, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t" \
+  "v_fmac_f32_dpp %1, %1, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
+        if constexpr (L == 16)
+          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
+              : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
+        if constexpr (L == 32)
+          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
+              SSK_STEP("6 row_bcast:15") : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15));
+        if constexpr (L == 64)
+          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
+              SSK_STEP("6 row_bcast:15") SSK_STEP("7 row_bcast:31")
+              : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15), "v"(m31));
+#undef SSK_STEP
+      }
+#pragma unroll
+      for (int a = 0; a < N; ++a) fine = fine && fabsf(s[a]) <= 3.4028235e38f;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
+#pragma unroll
+        for (int a = 0; a < N; ++a) s[a] = v[a][0];
+#define SSK_STEP(CTRL, M)                              \
+  _Pragma("unroll") for (int a = 0; a < N; ++a) {      \
+    const float o_ = dpp_or_0<CTRL>(s[a]);             \
+    s[a] += (M) != 0.f ? o_ : 0.f;                     \
+  }
+        SSK_STEP(0x111, m1)
+        SSK_STEP(0x112, m2)
+        SSK_STEP(0x114, m4)
+        SSK_STEP(0x118, m8)
+        if constexpr (L >= 32) { SSK_STEP(0x142, m15) }
+        if constexpr (L >= 64) { SSK_STEP(0x143, m31) }
+#undef SSK_STEP
+      }
+#pragma unroll
+      for (int a = 0; a < N; ++a) v[a][0] = read_lane(s[a], last);
     } else {
       float out[N][K] = {};
       for (int en = 0; en < n; ++en)
@@ -332,8 +392,9 @@ struct Row {
         v[k][c] = p && e[k] < entries && c < hi[k] ? p[f0[k] + field(k, c)] : 1.f;
   }
 
-  // The checkpoint of a row: int8 values at q, exponent bytes at b; of the chunks of the first `entries` entries.
-  __device__ __forceinline__ void pack(const f8 (&x)[K], int8_t* q, uint8_t* b, int entries, bool on) const {
+  // The checkpoint of row r: int8 values at q, exponent bytes at b; of the chunks of the first `entries` entries.
+  __device__ __forceinline__ void pack(const f8 (&x)[K], int8_t* q0, uint8_t* b0, int r, int C, int B, int entries,
+                                       bool on) const {
     uint32_t amax[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -377,12 +438,13 @@ struct Row {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if (!on || hi[k] == 0 || e[k] >= entries) continue;
+      int8_t* q = q0 + (uint32_t)(__umul24(r, C) + start[k]);
       const int byte = pack_byte(amax[k]);
-      const float inv = pack_inverse(byte);
+      const float scale = pack_inverse(byte);
       // 1.5 2^23 + v has v, rounded to nearest even, in its low bits
       uint32_t w[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) w[c] = byte == 255 ? 0u : __float_as_uint(fmaf(x[k][c], inv, 12582912.f));
+      for (int c = 0; c < 8; ++c) w[c] = byte == 255 ? 0u : __float_as_uint(fmaf(x[k][c], scale, 12582912.f));
       if (!RAG || (lo[k] == 0 && hi[k] == 8)) {
         u2 p;
 #pragma unroll
@@ -391,16 +453,89 @@ struct Row {
           const uint32_t h16 = __builtin_amdgcn_perm(w[4 * a + 3], w[4 * a + 2], 0x04000c0cu);
           p[a] = l16 | h16;
         }
-        *reinterpret_cast<u2_any*>(q + start[k]) = p;
+        *reinterpret_cast<u2_any*>(q) = p;
       } else {
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-          if (counts(k, c)) q[start[k] + c] = (int8_t)w[c];
+          if (counts(k, c)) q[c] = (int8_t)w[c];
       }
-      if (quad[k] == 0) b[blk[k]] = (uint8_t)byte;
+      if (quad[k] == 0) b0[(uint32_t)(__umul24(r, B) + blk[k])] = (uint8_t)byte;
     }
   }
 };
+
+// The gates of a row, shared out over its lanes: gate i + q L of the row has components [c0, c0 + d) of the fields.
+template <int L, int K, bool RAG>
+struct Gates {
+  static constexpr int Q = Row<L, K, RAG>::Q;
+  int c0[Q], d[Q], at[Q];  // d = 0: none; at: the gate's own channel
+
+  __device__ __forceinline__ void init(const SiteTab& t, int i) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int g = i + q * L;
+      c0[q] = d[q] = 0;
+      at[q] = t.C + g;
+#pragma unroll
+      for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {
+        const int f = g - t.gate0[en], dd = 2 * t.l[en] + 1;
+        const bool in = en < t.n_regular && t.l[en] > 0 && f >= 0 && f < t.mult[en];
+        c0[q] = in ? t.ch0[en] + f * dd : c0[q];
+        d[q] = in ? dd : d[q];
+      }
+    }
+  }
+
+  // buf[channel]: from the gates' inputs in their channels, their sigmoids in all components of what they gate.
+  __device__ __forceinline__ void open(float* buf, float (&s)[Q]) const {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) s[q] = d[q] ? buf[at[q]] : 0.f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (d[q] == 0) continue;
+      s[q] = sigmoid_of(s[q]);
+      float* b = buf + c0[q];
+      b[0] = b[1] = b[2] = s[q];
+      if (d[q] > 3) b[3] = b[4] = s[q];
+      if (d[q] > 5) b[5] = b[6] = s[q];
+      if (d[q] > 7) b[7] = b[8] = s[q];
+    }
+  }
+
+  // From the products dg * u in the components, the gates' gradients in their channels.
+  __device__ __forceinline__ void close(float* buf, const float (&s)[Q]) const {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (d[q] == 0) continue;
+      const float* b = buf + c0[q];
+      float v = (b[0] + b[1]) + b[2];
+      if (d[q] > 3) v += b[3] + b[4];
+      if (d[q] > 5) v += b[5] + b[6];
+      if (d[q] > 7) v += b[7] + b[8];
+      buf[at[q]] = v * (s[q] * (1.f - s[q]));
+    }
+  }
+};
+
+// 8 channels of a row in LDS; those past hi (where the chunk is no whole one) are left alone.
+template <int L, int K, bool RAG>
+__device__ __forceinline__ void lds_put(const Row<L, K, RAG>& w, int k, float* buf, f8 v) {
+  if constexpr (!RAG) {
+    *reinterpret_cast<f8*>(buf + w.start[k]) = v;
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      if (c < w.hi[k]) buf[w.start[k] + c] = v[c];
+  }
+}
+template <int L, int K, bool RAG>
+__device__ __forceinline__ f8 lds_get(const Row<L, K, RAG>& w, int k, const float* buf) {  // the buffer ends 8 past the row
+  if constexpr (!RAG) return *reinterpret_cast<const f8*>(buf + w.start[k]);
+  f8 v;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) v[c] = buf[w.start[k] + c];
+  return v;
+}
 
 // Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order, to out[channels];
 // lds holds one row of floats per row that the workgroup takes at a time.  All threads call it.

@@ -8,111 +8,119 @@
 namespace ssconv {
 namespace {
 
+constexpr f8 kZero = {0, 0, 0, 0, 0, 0, 0, 0};
+
 template <typename T, int L, int K, bool RAG>
-__global__ __launch_bounds__(kSiteNT) void tail_fwd_kernel(SiteTab t, TailArgs a) {
-  extern __shared__ float lds[];
+__global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_kernel(SiteTab t, TailArgs a, int lds_row) {
+  extern __shared__ __attribute__((aligned(32))) float lds[];
   using R = Row<L, K, RAG>;
   R w;
+  Gates<L, K, RAG> gates;
   w.init(t, t.n);
+  gates.init(t, w.i);
   const int C = t.C, S = t.ch0[t.n], By = t.b0[t.n], Bh = t.b0[t.n_regular], G = t.G;
-  float* sig = lds + ((threadIdx.x >> 6) * R::R + w.sub) * G;  // the row's gates
+  float* buf = lds + ((threadIdx.x >> 6) * R::R + w.sub) * lds_row;
   f8 gp[K], sc[K], gn[K];
   w.params(a.gain_post, gp, t.n);
   w.params(a.scale, sc, t.n_regular);
   w.params(a.gain_next, gn, t.n_regular);
   bool main[K];  // a chunk of the fields, not of the gates
+  int at[K];     // its place in a matrix without the gates
 #pragma unroll
-  for (int k = 0; k < K; ++k) main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
+  for (int k = 0; k < K; ++k) {
+    main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
+    at[k] = main[k] ? w.start[k] : 0;
+  }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
-  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < a.n; r0 += step) {
-    const bool on = r0 + w.sub < a.n;
-    const int64_t row = on ? r0 + w.sub : a.n - 1;
+  for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
+    const bool on = w.sub < a.n - r0;
+    const int row = w.row_of(a.n - r0);
     f8 y[K], h[K];
-    float r[K];
+    float r[K], sig[R::Q];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      y[k] = w.template load<T>((const T*)a.y.data + row * S, k);
-      h[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (main[k]) h[k] = w.template load<T>((const T*)a.h.data + row * C, k);
+      y[k] = w.template load<T>((const T*)a.y.data + r0 * S, row, S, k, w.start[k]);
+      h[k] = kZero;
+      if (!RAG || main[k]) h[k] = w.template load<T>((const T*)a.h.data + r0 * C, row, C, k, at[k]);
     }
-    if (a.yq) w.pack(y, a.yq + row * S, a.ye + row * By, t.n, on);
+    if (a.yq) w.pack(y, a.yq + r0 * S, a.ye + r0 * By, row, S, By, t.n, on);
     w.norm(y, r, a.eps);
-#pragma unroll
-    for (int k = 0; k < K; ++k) y[k] *= gp[k];
     if (G) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (w.hi[k] > 0 && !main[k])
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            if (c < w.hi[k]) sig[w.start[k] - C + c] = sigmoid_of(y[k][c]);
+        if (w.hi[k] > 0 && !main[k]) lds_put(w, k, buf, y[k] * gp[k]);
+      wave_lds_fence();
+      gates.open(buf, sig);
       wave_lds_fence();
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (!main[k]) continue;
+      const f8 f = G ? lds_get(w, k, buf) : kZero;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        float g = y[k][c];
-        if (w.scalar[k])
-          g = g <= 0.f ? 0.f : g;  // NaN stays
-        else if (!RAG || c < w.hi[k])
-          g *= sig[w.gate[k] + w.field(k, c)];
+        const float u = y[k][c] * gp[k][c];
+        const float g = w.scalar[k] ? (u <= 0.f ? 0.f : u) : f[c] * u;  // NaN stays
         h[k][c] = fmaf(sc[k][c], g, h[k][c]);
       }
       h[k] = round8<T>(h[k]);
-      if (on) w.template store<T>((T*)a.h_out + row * C, k, h[k]);
+      if (on && main[k]) w.template store<T>((T*)a.h_out + r0 * C, row, C, k, h[k]);
     }
     if (G) wave_lds_fence();
-    if (a.hq) w.pack(h, a.hq + row * C, a.he + row * Bh, t.n_regular, on);
+    if (a.hq) w.pack(h, a.hq + r0 * C, a.he + r0 * Bh, row, C, Bh, t.n_regular, on);
     if (a.x_out) {
       w.norm(h, r, a.eps);
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (on && main[k]) w.template store<T>((T*)a.x_out + row * C, k, h[k] * gn[k]);
+        if (on && main[k]) w.template store<T>((T*)a.x_out + r0 * C, row, C, k, h[k] * gn[k]);
     }
   }
 }
 
+// The parameters and their gradients' sums take 48 of a lane's registers.
 template <typename T, int L, int K, bool RAG>
-__global__ __launch_bounds__(kSiteNT) void tail_bwd_kernel(SiteTab t, TailArgs a) {
-  extern __shared__ float lds[];
+__global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_kernel(SiteTab t, TailArgs a, int lds_row) {
+  extern __shared__ __attribute__((aligned(32))) float lds[];
   using R = Row<L, K, RAG>;
   R w;
+  Gates<L, K, RAG> gates;
   w.init(t, t.n);
+  gates.init(t, w.i);
   const int C = t.C, S = t.ch0[t.n], By = t.b0[t.n], Bh = t.b0[t.n_regular], G = t.G;
-  float* sig = lds + ((threadIdx.x >> 6) * R::R + w.sub) * S;  // the row's gates, and behind them dg * u by channel
-  float* prod = sig + G;
+  float* buf = lds + ((threadIdx.x >> 6) * R::R + w.sub) * lds_row;
   f8 gp[K], sc[K], gn[K], acc_p[K], acc_s[K], acc_n[K];
   w.params(a.gain_post, gp, t.n);
   w.params(a.scale, sc, t.n_regular);
   w.params(a.gain_next, gn, t.n_regular);
-  const f8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   bool main[K];
+  int at[K], blk[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
-    acc_p[k] = acc_s[k] = acc_n[k] = zero;
+    at[k] = main[k] ? w.start[k] : 0;
+    blk[k] = main[k] ? w.blk[k] : 0;
+    acc_p[k] = acc_s[k] = acc_n[k] = kZero;
   }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
-  for (int64_t r0 = ((int64_t)blockIdx.x * (kSiteNT / 64) + (threadIdx.x >> 6)) * R::R; r0 < a.n; r0 += step) {
-    const bool on = r0 + w.sub < a.n;
-    const int64_t row = on ? r0 + w.sub : a.n - 1;
-    f8 y[K], h[K], dh[K], dx[K];
-    float r[K];
+  for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
+    const bool on = w.sub < a.n - r0;
+    const int row = w.row_of(a.n - r0);
+    f8 y[K], dh[K];
+    float r[K], sig[R::Q];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      y[k] = a.y.exps ? w.load_packed((const int8_t*)a.y.data + row * S, a.y.exps + row * By, k)
-                      : w.template load<T>((const T*)a.y.data + row * S, k);
-      h[k] = dh[k] = dx[k] = zero;
-      if (!main[k]) continue;
-      dh[k] = w.template load<T>((const T*)a.dh + row * C, k);
-      if (!a.dx) continue;
-      dx[k] = w.template load<T>((const T*)a.dx + row * C, k);
-      h[k] = a.h.exps ? w.load_packed((const int8_t*)a.h.data + row * C, a.h.exps + row * Bh, k)
-                      : w.template load<T>((const T*)a.h.data + row * C, k);
+      y[k] = w.template load_rows<T>(a.y, r0, row, S, By, k, w.start[k], w.blk[k]);
+      dh[k] = kZero;
+      if (!RAG || main[k]) dh[k] = w.template load<T>((const T*)a.dh + r0 * C, row, C, k, at[k]);
     }
     if (a.dx) {
+      f8 h[K], dx[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        h[k] = dx[k] = kZero;
+        if (RAG && !main[k]) continue;
+        dx[k] = w.template load<T>((const T*)a.dx + r0 * C, row, C, k, at[k]);
+        h[k] = w.template load_rows<T>(a.h, r0, row, C, Bh, k, at[k], blk[k]);
+      }
       w.norm(h, r, a.eps);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
@@ -125,53 +133,40 @@ __global__ __launch_bounds__(kSiteNT) void tail_bwd_kernel(SiteTab t, TailArgs a
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (on && main[k]) w.template store<T>((T*)a.dh_in + row * C, k, dh[k]);
+      if (on && main[k]) w.template store<T>((T*)a.dh_in + r0 * C, row, C, k, dh[k]);
     w.norm(y, r, a.eps);
     if (G) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (w.hi[k] > 0 && !main[k])
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            if (c < w.hi[k]) sig[w.start[k] - C + c] = sigmoid_of(y[k][c] * gp[k][c]);
+        if (w.hi[k] > 0 && !main[k]) lds_put(w, k, buf, y[k] * gp[k]);
+      wave_lds_fence();
+      gates.open(buf, sig);
       wave_lds_fence();
     }
     f8 du[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      du[k] = zero;
-      if (!main[k]) continue;
+      const f8 f = G ? lds_get(w, k, buf) : kZero;
+      f8 gated, prod;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const float u = y[k][c] * gp[k][c];
-        float f = u > 0.f ? 1.f : 0.f;
-        if (!w.scalar[k] && (!RAG || c < w.hi[k])) f = sig[w.gate[k] + w.field(k, c)];
+        const float on_off = u > 0.f ? 1.f : 0.f, fc = w.scalar[k] ? on_off : f[c];
         const float dg = sc[k][c] * dh[k][c];
-        if (on) acc_s[k][c] = fmaf(dh[k][c], f * u, acc_s[k][c]);
-        du[k][c] = dg * f;
-        if (!w.scalar[k] && (!RAG || c < w.hi[k])) prod[w.start[k] + c] = dg * u;
+        gated[c] = dh[k][c] * (fc * u);
+        du[k][c] = dg * fc;
+        prod[c] = dg * u;
       }
+      if (on) acc_s[k] += gated;
+      if (G && main[k]) lds_put(w, k, buf, prod);
     }
     if (G) {
-      // a field's products make its gate's gradient; the fields of the row are shared out over its lanes
       wave_lds_fence();
-      for (int e = 0; e < t.n_regular; ++e) {
-        if (t.l[e] == 0) continue;
-        const int d = 2 * t.l[e] + 1;
-        for (int f = w.i; f < t.mult[e]; f += L) {
-          float s = 0.f;
-          for (int c = 0; c < d; ++c) s += prod[t.ch0[e] + f * d + c];
-          const float sg = sig[t.gate0[e] + f];
-          sig[t.gate0[e] + f] = s * (sg * (1.f - sg));
-        }
-      }
+      gates.close(buf, sig);
       wave_lds_fence();
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (w.hi[k] > 0 && !main[k])
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            if (c < w.hi[k]) du[k][c] = sig[w.start[k] - C + c];
+        if (w.hi[k] > 0 && !main[k]) du[k] = lds_get(w, k, buf);
       wave_lds_fence();
     }
 #pragma unroll
@@ -182,7 +177,7 @@ __global__ __launch_bounds__(kSiteNT) void tail_bwd_kernel(SiteTab t, TailArgs a
     w.norm_back(y, r, du);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (on) w.template store<T>((T*)a.dy + row * S, k, du[k]);
+      if (on) w.template store<T>((T*)a.dy + r0 * S, row, S, k, du[k]);
   }
   if (a.part) {
     float* out = a.part + (int64_t)blockIdx.x * (S + 2 * C);
@@ -195,10 +190,11 @@ __global__ __launch_bounds__(kSiteNT) void tail_bwd_kernel(SiteTab t, TailArgs a
 }  // namespace
 
 int launch_tail_fwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStream_t st) {
-  const unsigned nb = site_blocks(t, a.n, kFwdPerCu);
-  const size_t lds = (size_t)site_rows(t) * t.G * 4;
+  const unsigned nb = site_blocks(t, a.n, tail_fwd_per_cu);
+  const int lds_row = site_lds_row(t);
+  const size_t lds = t.G ? (size_t)site_rows(t) * lds_row * 4 : 0;
   auto go = [&](auto kernel) {
-    kernel<<<nb, kSiteNT, lds, st>>>(t, a);
+    kernel<<<nb, kSiteNT, lds, st>>>(t, a, lds_row);
     SSC_HIP(hipGetLastError());
     return (int)SSCONV_OK;
   };
@@ -209,10 +205,11 @@ int launch_tail_fwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStr
 }
 
 int launch_tail_bwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStream_t st) {
-  const unsigned nb = site_blocks(t, a.n, kBwdPerCu);
-  const size_t lds = (size_t)site_rows(t) * t.ch0[t.n] * 4;
+  const unsigned nb = site_blocks(t, a.n, tail_bwd_per_cu);
+  const int lds_row = site_lds_row(t);
+  const size_t lds = (size_t)site_rows(t) * lds_row * 4;
   auto go = [&](auto kernel) {
-    kernel<<<nb, kSiteNT, lds, st>>>(t, a);
+    kernel<<<nb, kSiteNT, lds, st>>>(t, a, lds_row);
     SSC_HIP(hipGetLastError());
     return (int)SSCONV_OK;
   };
