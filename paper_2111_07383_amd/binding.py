@@ -9,6 +9,7 @@ import ctypes
 from contextlib import nullcontext
 from ctypes import byref, c_float, c_int, c_int64, c_void_p
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import Optional, Sequence, Tuple, Union
 
 import numpy as np
@@ -345,13 +346,9 @@ def norm_backward(fields: FieldList, x: torch.Tensor, dy: torch.Tensor, eps: flo
     return dx
 
 
-def _here(*tensors):
-    """The calls below launch on the current device: their tensors have to be there."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
-
+# ---- norm of a site, residual tail, checkpoints ---------------------------------------------
+# A call on a few sites is over in a few microseconds, so what a field list says is looked up once and the arguments'
+# checks take one comparison each where they pass.
 
 def _on(stream):
     """Results and scratch of a call on a given stream come from that stream's memory: a block of another stream may
@@ -359,27 +356,55 @@ def _on(stream):
     return nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def _field_list(fields: FieldList) -> Tuple[Tuple[int, int], ...]:
+class _Table:
+    """A field list: its C structure, channels, fields, checkpoint blocks (0: the library refuses the list)."""
+
+    def __init__(self, fields):
+        self.fields = fields
+        self.struct = make_fields(fields)
+        self.ref = byref(self.struct)
+        self.C = n_channels(fields)
+        self.F = sum(m for _, m in fields)
+        self.blocks = int(lib().ssconv_packed_blocks(self.ref))
+        self.error = "" if self.blocks else lib().ssconv_last_error().decode()
+        self.gates = sum(m for l, m in fields if l > 0)
+        self.full_fields = fields + (((0, self.gates),) if self.gates else ())
+        self._full = None
+
+    @property
+    def full(self) -> "_Table":
+        """The fields with their gates."""
+        if self._full is None:
+            self._full = _table(self.full_fields)
+        return self._full
+
+
+@lru_cache(maxsize=256)
+def _table_of(fields) -> _Table:
     fields = tuple((int(l), int(m)) for l, m in fields)
     if not 1 <= len(fields) <= MAX_ENTRIES:
         raise ValueError(f"a field list has 1 to {MAX_ENTRIES} entries")
-    return fields
+    return _Table(fields)
+
+
+def _table(fields: FieldList) -> _Table:
+    try:
+        return _table_of(fields)
+    except TypeError:                       # a list, or lists in it
+        return _table_of(tuple(tuple(e) for e in fields))
 
 
 def gate_fields(fields: FieldList) -> Tuple[Tuple[int, int], ...]:
     """The fields with their gate channels (one scalar per field of order > 0) as one more entry."""
-    fields = _field_list(fields)
-    g = sum(m for l, m in fields if l > 0)
-    return fields + (((0, g),) if g else ())
+    return _table(fields).full_fields
 
 
 def packed_blocks(fields: FieldList) -> int:
     """Exponent bytes of a row of a checkpoint (ssconv_packed_blocks); raises for a bad list."""
-    f = make_fields(_field_list(fields))
-    b = int(lib().ssconv_packed_blocks(byref(f)))
-    if b == 0:
-        raise ValueError(f"bad field list {tuple(fields)}: " + lib().ssconv_last_error().decode())
-    return b
+    t = _table(fields)
+    if t.blocks == 0:
+        raise ValueError(f"bad field list {t.fields}: {t.error}")
+    return t.blocks
 
 
 @dataclass
@@ -404,80 +429,90 @@ class Packed:
 
     @staticmethod
     def empty(fields: FieldList, n: int, device) -> "Packed":
-        fields = _field_list(fields)
-        return Packed(fields, torch.empty((n, n_channels(fields)), dtype=torch.int8, device=device),
-                      torch.empty((n, packed_blocks(fields)), dtype=torch.uint8, device=device))
+        t = _table(fields)
+        return Packed(t.fields, torch.empty((n, t.C), dtype=torch.int8, device=device),
+                      torch.empty((n, packed_blocks(t.fields)), dtype=torch.uint8, device=device))
 
 
-def _need_packed(p: Packed, name: str, fields: FieldList, n: Optional[int] = None):
-    fields = _field_list(fields)
-    if _field_list(p.fields) != fields:
-        raise ValueError(f"{name} is a checkpoint of fields {tuple(p.fields)}, not {fields}")
-    n = p.q.shape[0] if n is None else n
-    _need(p.q, f"{name}.q", torch.int8, (n, n_channels(fields)))
-    _need(p.exps, f"{name}.exps", torch.uint8, (n, packed_blocks(fields)))
-    _here(p.q, p.exps)
+def _check(t: torch.Tensor, name: str, dev: int, dtype, shape):
+    """A contiguous tensor of this type and shape on the current device."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return
+    _need(t, name, dtype, shape)
+    raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
 
 
-def _need_rows(t: torch.Tensor, name: str, channels: int, dtype=None, n: Optional[int] = None):
-    _need(t, name, dtype)
-    _dtype(t)
-    if t.dim() != 2 or t.shape[1] != channels or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name} must be [{'n' if n is None else n}, {channels}], got {tuple(t.shape)}")
-    _here(t)
+def _rows_of(x: torch.Tensor, name: str, dev: int, C: int) -> int:
+    """Rows of a feature matrix of C channels."""
+    if x.dim() != 2 or x.shape[1] != C:
+        _need(x, name)
+        raise ValueError(f"{name} must be [n, {C}], got {tuple(x.shape)}")
+    n = x.shape[0]
+    _dtype(x)
+    _check(x, name, dev, x.dtype, (n, C))
+    return n
 
 
-def _need_params(t: Optional[torch.Tensor], name: str, fields: FieldList):
-    if t is not None:
-        _need(t, name, torch.float32, (sum(int(m) for _, m in fields),))
-        _here(t)
+def _check_packed(p: Packed, name: str, dev: int, t: _Table, n: int):
+    if p.fields is not t.fields and _table(p.fields).fields != t.fields:
+        raise ValueError(f"{name} is a checkpoint of fields {tuple(p.fields)}, not {t.fields}")
+    _check(p.q, name + ".q", dev, torch.int8, (n, t.C))
+    _check(p.exps, name + ".exps", dev, torch.uint8, (n, packed_blocks(t.fields) if t.blocks == 0 else t.blocks))
 
 
-def _rows(x: Union[torch.Tensor, Packed]) -> Rows:
+def _check_rows(x, name: str, dev: int, t: _Table, n: int, dtype) -> Rows:
+    """Rows in ``dtype`` or a checkpoint of them, as the library takes them."""
     if isinstance(x, Packed):
+        _check_packed(x, name, dev, t, n)
         return Rows(x.q.data_ptr(), x.exps.data_ptr())
-    return Rows(0 if x is None else x.data_ptr(), None)
+    _check(x, name, dev, dtype, (n, t.C))
+    return Rows(x.data_ptr(), None)
 
 
-def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+def _param(p: Optional[torch.Tensor], name: str, dev: int, t: _Table):
+    if p is None:
+        return None
+    _check(p, name, dev, torch.float32, (t.F,))
+    return p.data_ptr()
+
+
+def _workspace(ws: Optional[torch.Tensor], need: int, dev: int, device) -> torch.Tensor:
     if ws is None:
-        return torch.empty((max(need, 256),), dtype=torch.uint8, device=device)
-    _need(ws, "workspace", torch.uint8)
-    _here(ws)
+        return torch.empty((need or 256,), dtype=torch.uint8, device=device)
+    _check(ws, "workspace", dev, torch.uint8, (ws.numel(),))
     if ws.numel() < need:
         raise ValueError(f"workspace must hold {need} bytes, got {ws.numel()}")
     return ws
 
 
-def _new_or(out: Optional[torch.Tensor], name: str, like: torch.Tensor, channels: int) -> torch.Tensor:
-    if out is None:
-        return torch.empty((like.shape[0], channels), dtype=like.dtype, device=like.device)
-    _need_rows(out, name, channels, like.dtype, like.shape[0])
-    return out
+def _raw_stream(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def pack(fields: FieldList, x: torch.Tensor, stream=None) -> Packed:
     """An 8-bit checkpoint of x [n, C]."""
-    fields = _field_list(fields)
-    _need_rows(x, "x", n_channels(fields))
+    t, dev = _table(fields), torch.cuda.current_device()
+    n = _rows_of(x, "x", dev, t.C)
+    blocks = packed_blocks(t.fields) if t.blocks == 0 else t.blocks
     with _on(stream):
-        p = Packed.empty(fields, x.shape[0], x.device)
-    f = make_fields(fields)
-    check(lib().ssconv_pack(byref(f), _ptr(x), _dtype(x), x.shape[0], _ptr(p.q), _ptr(p.exps), _stream(stream)),
+        q = torch.empty((n, t.C), dtype=torch.int8, device=x.device)
+        exps = torch.empty((n, blocks), dtype=torch.uint8, device=x.device)
+    check(lib().ssconv_pack(t.ref, x.data_ptr(), _dtype(x), n, q.data_ptr(), exps.data_ptr(), _raw_stream(stream, dev)),
           "ssconv_pack")
-    return p
+    return Packed(t.fields, q, exps)
 
 
 def unpack(p: Packed, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values that a checkpoint stands for (exact in either type)."""
-    _need_packed(p, "p", p.fields)
+    t, dev = _table(p.fields), torch.cuda.current_device()
+    n = p.q.shape[0]
+    _check_packed(p, "p", dev, t, n)
     if out is None:
         with _on(stream):
-            out = torch.empty(p.shape, dtype=dtype, device=p.device)
-    _need_rows(out, "out", p.shape[1], dtype, p.shape[0])
-    f = make_fields(p.fields)
-    check(lib().ssconv_unpack(byref(f), _ptr(p.q), _ptr(p.exps), p.shape[0], _dtype(out), _ptr(out), _stream(stream)),
-          "ssconv_unpack")
+            out = torch.empty((n, t.C), dtype=dtype, device=p.q.device)
+    _check(out, "out", dev, dtype, (n, t.C))
+    check(lib().ssconv_unpack(t.ref, p.q.data_ptr(), p.exps.data_ptr(), n, _dtype(out), out.data_ptr(),
+                              _raw_stream(stream, dev)), "ssconv_unpack")
     return out
 
 
@@ -485,31 +520,30 @@ def site_norm_forward(fields: FieldList, x: Union[torch.Tensor, Packed], gain: O
                       eps: float = NORM_EPS, out: Optional[torch.Tensor] = None, checkpoint: bool = False,
                       dtype: Optional[torch.dtype] = None, stream=None):
     """ssconv_site_norm_forward: the norm of every site of x [n, C] (or of a checkpoint; ``dtype`` is then the
-    result's, bf16 unless given).  With ``checkpoint``: (y, checkpoint of x)."""
-    fields = _field_list(fields)
-    C = n_channels(fields)
-    _need_params(gain, "gain", fields)
+    result's, bf16 unless given).  With ``checkpoint``: (y, checkpoint of x).  ``out`` may be x."""
+    t, dev = _table(fields), torch.cuda.current_device()
+    g = _param(gain, "gain", dev, t)
     if isinstance(x, Packed):
         if checkpoint:
             raise ValueError("x is a checkpoint already")
-        _need_packed(x, "x", fields)
+        n, device = x.q.shape[0], x.q.device
         dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
-        if out is None:
-            with _on(stream):
-                out = torch.empty(x.shape, dtype=dtype, device=x.device)
-        _need_rows(out, "out", C, dtype, x.shape[0])
+        r = _check_rows(x, "x", dev, t, n, None)
     else:
-        _need_rows(x, "x", C)
+        n, device = _rows_of(x, "x", dev, t.C), x.device
         if dtype is not None and dtype != x.dtype:
             raise TypeError(f"the result of {x.dtype} rows is {x.dtype}, not {dtype}")
-        with _on(stream):
-            out = _new_or(out, "out", x, C)
+        dtype = x.dtype
+        r = Rows(x.data_ptr(), None)
     with _on(stream):
-        p = Packed.empty(fields, x.shape[0], x.device) if checkpoint else None
-    f, r = make_fields(fields), _rows(x)
-    check(lib().ssconv_site_norm_forward(byref(f), byref(r), _dtype(out), x.shape[0], float(eps), _ptr(gain), _ptr(out),
-                                         _ptr(p.q if p else None), _ptr(p.exps if p else None), _stream(stream)),
-          "ssconv_site_norm_forward")
+        if out is None:
+            out = torch.empty((n, t.C), dtype=dtype, device=device)
+        else:
+            _check(out, "out", dev, dtype, (n, t.C))
+        p = Packed.empty(t.fields, n, device) if checkpoint else None
+    check(lib().ssconv_site_norm_forward(t.ref, byref(r), _dtype(out), n, eps, g, out.data_ptr(),
+                                         p.q.data_ptr() if p else None, p.exps.data_ptr() if p else None,
+                                         _raw_stream(stream, dev)), "ssconv_site_norm_forward")
     return (out, p) if checkpoint else out
 
 
@@ -517,27 +551,29 @@ def site_norm_backward(fields: FieldList, x: Union[torch.Tensor, Packed], dy: to
                        gain: Optional[torch.Tensor] = None, eps: float = NORM_EPS,
                        dres: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None, stream=None):
-    """ssconv_site_norm_backward: (gradient of x plus dres, gradient of the gain or None without one)."""
-    fields = _field_list(fields)
-    C = n_channels(fields)
-    _need_rows(dy, "dy", C)
-    n = dy.shape[0]
-    if isinstance(x, Packed):
-        _need_packed(x, "x", fields, n)
-    else:
-        _need_rows(x, "x", C, dy.dtype, n)
+    """ssconv_site_norm_backward: (gradient of x plus dres, gradient of the gain or None without one).  ``out`` may be
+    dy or dres."""
+    t, dev = _table(fields), torch.cuda.current_device()
+    n, dtype = _rows_of(dy, "dy", dev, t.C), dy.dtype
+    shape = (n, t.C)
+    r = _check_rows(x, "x", dev, t, n, dtype)
     if dres is not None:
-        _need_rows(dres, "dres", C, dy.dtype, n)
-    _need_params(gain, "gain", fields)
-    f, r = make_fields(fields), _rows(x)
+        _check(dres, "dres", dev, dtype, shape)
+    g = _param(gain, "gain", dev, t)
     with _on(stream):
-        out = _new_or(out, "out", dy, C)
-        dgain = torch.empty_like(gain) if gain is not None else None
-        need = lib().ssconv_site_norm_workspace_size(byref(f), n) if gain is not None else 0
-        ws = _workspace(workspace, need, dy.device)
-    check(lib().ssconv_site_norm_backward(byref(f), byref(r), _ptr(dy), _ptr(dres), _dtype(dy), n, float(eps),
-                                          _ptr(gain), _ptr(out), _ptr(dgain), _ptr(ws), ws.numel(), _stream(stream)),
-          "ssconv_site_norm_backward")
+        if out is None:
+            out = torch.empty_like(dy)
+        else:
+            _check(out, "out", dev, dtype, shape)
+        dgain = ws = None
+        if gain is not None:
+            dgain = torch.empty_like(gain)
+            ws = _workspace(workspace, lib().ssconv_site_norm_workspace_size(t.ref, n), dev, dy.device)
+    check(lib().ssconv_site_norm_backward(t.ref, byref(r), dy.data_ptr(), None if dres is None else dres.data_ptr(),
+                                          _dtype(dy), n, eps, g, out.data_ptr(),
+                                          None if dgain is None else dgain.data_ptr(),
+                                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                          _raw_stream(stream, dev)), "ssconv_site_norm_backward")
     return out, dgain
 
 
@@ -548,28 +584,28 @@ def residual_forward(fields: FieldList, y: torch.Tensor, h: torch.Tensor, scale:
     """ssconv_residual_forward: (h_out, x_out, checkpoint of y, checkpoint of h_out) of the convolution output y
     [n, C + G] and the residual stream h [n, C]; x_out is None without ``next_norm``, the checkpoints without
     ``checkpoint`` (and the one of h_out without ``next_norm``, whose backward alone reads it).  ``out`` may be h."""
-    fields = _field_list(fields)
-    full, C = gate_fields(fields), n_channels(fields)
-    _need_rows(h, "h", C)
-    n = h.shape[0]
-    _need_rows(y, "y", n_channels(full), h.dtype, n)
-    _need_params(scale, "scale", fields)
-    _need_params(gain_post, "gain_post", full)
-    _need_params(gain_next, "gain_next", fields)
-    if gain_next is not None and not next_norm:
+    t, dev = _table(fields), torch.cuda.current_device()
+    full = t.full
+    n, dtype = _rows_of(h, "h", dev, t.C), h.dtype
+    shape = (n, t.C)
+    _check(y, "y", dev, dtype, (n, full.C))
+    s, gp, gn = _param(scale, "scale", dev, t), _param(gain_post, "gain_post", dev, full), _param(gain_next, "gain_next", dev, t)
+    if gn is not None and not next_norm:
         raise ValueError("gain_next without the next norm")
     with _on(stream):
-        h_out = _new_or(out, "out", h, C)
+        if out is None:
+            out = torch.empty_like(h)
+        else:
+            _check(out, "out", dev, dtype, shape)
         x_out = torch.empty_like(h) if next_norm else None
-        yp = Packed.empty(full, n, h.device) if checkpoint else None
-        hp = Packed.empty(fields, n, h.device) if checkpoint and next_norm else None
-    f = make_fields(fields)
-    check(lib().ssconv_residual_forward(byref(f), _ptr(y), _ptr(h), _dtype(h), n, float(eps), _ptr(gain_post),
-                                        _ptr(scale), _ptr(gain_next), _ptr(h_out), _ptr(x_out),
-                                        _ptr(yp.q if yp else None), _ptr(yp.exps if yp else None),
-                                        _ptr(hp.q if hp else None), _ptr(hp.exps if hp else None), _stream(stream)),
-          "ssconv_residual_forward")
-    return h_out, x_out, yp, hp
+        yp = Packed.empty(full.fields, n, h.device) if checkpoint else None
+        hp = Packed.empty(t.fields, n, h.device) if checkpoint and next_norm else None
+    check(lib().ssconv_residual_forward(t.ref, y.data_ptr(), h.data_ptr(), _dtype(h), n, eps, gp, s, gn, out.data_ptr(),
+                                        x_out.data_ptr() if next_norm else None,
+                                        yp.q.data_ptr() if yp else None, yp.exps.data_ptr() if yp else None,
+                                        hp.q.data_ptr() if hp else None, hp.exps.data_ptr() if hp else None,
+                                        _raw_stream(stream, dev)), "ssconv_residual_forward")
+    return out, x_out, yp, hp
 
 
 def residual_backward(fields: FieldList, y: Union[torch.Tensor, Packed],
@@ -580,39 +616,35 @@ def residual_backward(fields: FieldList, y: Union[torch.Tensor, Packed],
     """ssconv_residual_backward: (dy, gradient of h, dscale, dgain_post, dgain_next) from the gradients dh of h_out and
     dx of x_out (None without the next norm; h_out may then be None); y and h_out as rows or as checkpoints.  The
     gradient of a parameter that is None is None."""
-    fields = _field_list(fields)
-    full, C = gate_fields(fields), n_channels(fields)
-    _need_rows(dh, "dh", C)
-    n, S = dh.shape[0], n_channels(full)
-    if isinstance(y, Packed):
-        _need_packed(y, "y", full, n)
-    else:
-        _need_rows(y, "y", S, dh.dtype, n)
+    t, dev = _table(fields), torch.cuda.current_device()
+    full = t.full
+    n, dtype = _rows_of(dh, "dh", dev, t.C), dh.dtype
+    yr = _check_rows(y, "y", dev, full, n, dtype)
+    hr = Rows()
     if dx is not None:
-        _need_rows(dx, "dx", C, dh.dtype, n)
+        _check(dx, "dx", dev, dtype, (n, t.C))
         if h_out is None:
             raise ValueError("dx needs h_out")
-        if isinstance(h_out, Packed):
-            _need_packed(h_out, "h_out", fields, n)
-        else:
-            _need_rows(h_out, "h_out", C, dh.dtype, n)
+        hr = _check_rows(h_out, "h_out", dev, t, n, dtype)
     elif gain_next is not None:
         raise ValueError("gain_next without dx")
-    _need_params(scale, "scale", fields)
-    _need_params(gain_post, "gain_post", full)
-    _need_params(gain_next, "gain_next", fields)
-    f, yr, hr = make_fields(fields), _rows(y), _rows(h_out)
+    s, gp, gn = _param(scale, "scale", dev, t), _param(gain_post, "gain_post", dev, full), _param(gain_next, "gain_next", dev, t)
     with _on(stream):
-        dy = torch.empty((n, S), dtype=dh.dtype, device=dh.device)
+        dy = torch.empty((n, full.C), dtype=dtype, device=dh.device)
         dh_in = torch.empty_like(dh)
-        grads = [torch.empty_like(p) if p is not None else None for p in (scale, gain_post, gain_next)]
-        need = lib().ssconv_residual_workspace_size(byref(f), n) if any(g is not None for g in grads) else 0
-        ws = _workspace(workspace, need, dh.device)
-    check(lib().ssconv_residual_backward(byref(f), byref(yr), byref(hr), _ptr(dh), _ptr(dx), _dtype(dh), n, float(eps),
-                                         _ptr(gain_post), _ptr(scale), _ptr(gain_next), _ptr(dy), _ptr(dh_in),
-                                         _ptr(grads[1]), _ptr(grads[0]), _ptr(grads[2]), _ptr(ws), ws.numel(),
-                                         _stream(stream)), "ssconv_residual_backward")
-    return (dy, dh_in, *grads)
+        ds = None if s is None else torch.empty_like(scale)
+        dp = None if gp is None else torch.empty_like(gain_post)
+        dn = None if gn is None else torch.empty_like(gain_next)
+        ws = None
+        if s is not None or gp is not None or gn is not None:
+            ws = _workspace(workspace, lib().ssconv_residual_workspace_size(t.ref, n), dev, dh.device)
+    check(lib().ssconv_residual_backward(t.ref, byref(yr), byref(hr), dh.data_ptr(),
+                                         None if dx is None else dx.data_ptr(), _dtype(dh), n, eps, gp, s, gn,
+                                         dy.data_ptr(), dh_in.data_ptr(), None if dp is None else dp.data_ptr(),
+                                         None if ds is None else ds.data_ptr(), None if dn is None else dn.data_ptr(),
+                                         None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                         _raw_stream(stream, dev)), "ssconv_residual_backward")
+    return dy, dh_in, ds, dp, dn
 
 
 def backward_packed_workspace_size(rb: Rulebook, dtype: torch.dtype, cin: int, cout: int) -> int:
@@ -626,15 +658,16 @@ def backward_packed(feats: Packed, grad_out: torch.Tensor, rb: Rulebook, W: torc
                     workspace: Optional[torch.Tensor] = None, stream=None):
     """ssconv_backward_packed: ``backward`` of a convolution whose input is the checkpoint ``feats`` (``norm``: the site
     norm of it, with ``gain``)."""
-    fields = _field_list(feats.fields)
-    _need_packed(feats, "feats", fields, rb.n_in)
-    _need(W, "W", grad_out.dtype)
-    if W.dim() != 3 or W.shape[0] != rb.K or W.shape[2] != n_channels(fields):
-        raise ValueError(f"W must be [{rb.K}, cout, {n_channels(fields)}], got {tuple(W.shape)}")
+    t, dev = _table(feats.fields), torch.cuda.current_device()
+    _check_packed(feats, "feats", dev, t, rb.n_in)
+    if W.dim() != 3 or W.shape[0] != rb.K or W.shape[2] != t.C:
+        raise ValueError(f"W must be [{rb.K}, cout, {t.C}], got {tuple(W.shape)}")
     K, cout, cin = W.shape
-    _need_rows(grad_out, "grad_out", cout, None, rb.n_out)
-    _need_params(gain, "gain", fields)
-    if gain is not None and not norm:
+    _check(W, "W", dev, grad_out.dtype, (K, cout, cin))
+    _dtype(grad_out)
+    _check(grad_out, "grad_out", dev, grad_out.dtype, (rb.n_out, cout))
+    g = _param(gain, "gain", dev, t)
+    if g is not None and not norm:
         raise ValueError("gain without the norm")
     coeffs = 0
     if need_coeffs:
@@ -643,19 +676,17 @@ def backward_packed(feats: Packed, grad_out: torch.Tensor, rb: Rulebook, W: torc
         floats, coeffs = basis_info(desc)
         if n_coeff is not None and n_coeff != coeffs:
             raise ValueError(f"the layer has {coeffs} coefficients, not {n_coeff}")
-        _need(basis, "basis", torch.float32)
+        _check(basis, "basis", dev, torch.float32, basis.shape)
         if basis.numel() < floats:
             raise ValueError(f"basis needs {floats} floats")
-    _here(W, grad_out, basis)
     with _on(stream):
         gf = torch.empty((rb.n_in, cin), dtype=grad_out.dtype, device=grad_out.device) if need_feats else None
         gc = torch.empty((coeffs,), dtype=torch.float32, device=grad_out.device) if need_coeffs else None
-        ws = _workspace(workspace, backward_packed_workspace_size(rb, grad_out.dtype, cin, cout), grad_out.device)
-    f = make_fields(fields)
-    check(lib().ssconv_backward_packed(byref(f), _ptr(feats.q), _ptr(feats.exps), int(bool(norm)), float(eps),
-                                       _ptr(gain), _ptr(grad_out), _dtype(grad_out), cout, rb.handle, _ptr(W),
+        ws = _workspace(workspace, backward_packed_workspace_size(rb, grad_out.dtype, cin, cout), dev, grad_out.device)
+    check(lib().ssconv_backward_packed(t.ref, feats.q.data_ptr(), feats.exps.data_ptr(), int(bool(norm)), eps, g,
+                                       grad_out.data_ptr(), _dtype(grad_out), cout, rb.handle, W.data_ptr(),
                                        byref(desc) if desc is not None else None, _ptr(basis), _ptr(gf), _ptr(gc),
-                                       _ptr(ws), ws.numel(), _stream(stream)), "ssconv_backward_packed")
+                                       ws.data_ptr(), ws.numel(), _raw_stream(stream, dev)), "ssconv_backward_packed")
     return gf, gc
 
 

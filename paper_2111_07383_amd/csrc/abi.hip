@@ -113,17 +113,19 @@ extern "C" int ssconv_forward_noalloc(const void* feats, ssconv_dtype dtype, int
 extern "C" size_t ssconv_backward_workspace_size(ssconv_rulebook_t rb, ssconv_dtype dtype, int cin, int cout) {
   if (!rb || cin < 1 || cout < 1) return 0;
   if (rulebook_settle(rb) != SSCONV_OK) return 0;
-  return bwd_layout(rb, dtype, cin, cout).total;
+  return bwd_layout(rb, dtype, cin, cout, false).total;
 }
 
-extern "C" int ssconv_backward(const void* feats, const void* grad_out, ssconv_dtype dtype, int cin, int cout,
-                               ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc, const float* basis,
-                               void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes,
-                               hipStream_t stream) {
+// Checks and runs a backward call.  whole: with the largest tiles of the kernel gradient too, whose sums are in another
+// order; ssconv_backward keeps the order that it has always had.
+static int run_backward(const void* feats, const void* grad_out, ssconv_dtype dtype, int cin, int cout,
+                        ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc, const float* basis,
+                        void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes, bool whole,
+                        hipStream_t stream) {
   SSC_TRY(check_conv_args(feats, grad_out, dtype, cin, cout, rb, W));
   SSC_TRY(rulebook_settle(rb));
   if (grad_feats && !aligned16(grad_feats)) return fail(SSCONV_E_INVALID, "grad_feats must be 16-byte aligned");
-  const BwdLayout L = bwd_layout(rb, dtype, cin, cout);
+  const BwdLayout L = bwd_layout(rb, dtype, cin, cout, whole);
   if (!workspace || ws_bytes < L.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return fail(SSCONV_E_INVALID, "workspace must be 256-byte aligned and hold %zu bytes", L.total);
   if ((rb->n_out > 0 && !grad_out) || (rb->n_in > 0 && !feats)) return fail(SSCONV_E_INVALID, "NULL input buffer");
@@ -182,6 +184,14 @@ extern "C" int ssconv_backward(const void* feats, const void* grad_out, ssconv_d
   return rc;
 }
 
+extern "C" int ssconv_backward(const void* feats, const void* grad_out, ssconv_dtype dtype, int cin, int cout,
+                               ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc, const float* basis,
+                               void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes,
+                               hipStream_t stream) {
+  return run_backward(feats, grad_out, dtype, cin, cout, rb, W, desc, basis, grad_feats, grad_coeffs, workspace,
+                      ws_bytes, false, stream);
+}
+
 // ---------------------------------------------------------------------------
 // the gradient of a convolution whose input is kept as an 8-bit checkpoint
 // ---------------------------------------------------------------------------
@@ -192,12 +202,15 @@ size_t packed_rows_bytes(const ssconv_rulebook* rb, ssconv_dtype dtype, int cin)
 }  // namespace
 
 extern "C" size_t ssconv_backward_packed_workspace_size(ssconv_rulebook_t rb, ssconv_dtype dtype, int cin, int cout) {
-  const size_t b = ssconv_backward_workspace_size(rb, dtype, cin, cout);
-  return b == 0 ? 0 : b + packed_rows_bytes(rb, dtype, cin);
+  if (!rb || cin < 1 || cout < 1) return 0;
+  if (rulebook_settle(rb) != SSCONV_OK) return 0;
+  return bwd_layout(rb, dtype, cin, cout, true).total + packed_rows_bytes(rb, dtype, cin);
 }
 
-// The rows are expanded in front of the kernel gradient rather than in its loads: a row is read by about
-// n_pairs / n_in pairs of every unit's lists, and would be normed and rounded that often.
+// The rows are expanded in front of the kernel gradient rather than in its loads: a row is read by n_pairs / n_in
+// pairs and would be normed, or at least scaled and rounded, that often, 20 VALU instructions for the 8 values of a
+// lane where a step of the kernel has 56 MFMAs for 7 such operands (expansion of 103.7k sites of 208 channels: 12 of
+// the call's us).
 extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8_t* q, const uint8_t* exps, int norm,
                                       double eps, const float* gain, const void* grad_out, ssconv_dtype dtype, int cout,
                                       ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc,
@@ -218,6 +231,6 @@ extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8
   const size_t used = packed_rows_bytes(rb, dtype, t.C);
   if (grad_coeffs && rb->n_in > 0)
     SSC_TRY(expand_packed(t, dtype, q, exps, rb->n_in, norm != 0, (float)eps, gain, rows, stream));
-  return ssconv_backward(rows, grad_out, dtype, t.C, cout, rb, W, desc, basis, grad_feats, grad_coeffs,
-                         (char*)workspace + used, ws_bytes - used, stream);
+  return run_backward(rows, grad_out, dtype, t.C, cout, rb, W, desc, basis, grad_feats, grad_coeffs,
+                      (char*)workspace + used, ws_bytes - used, true, stream);
 }

@@ -506,7 +506,7 @@ static size_t kgrad_copy_bytes(ssconv_dtype dt, int64_t n, int c) {
 static bool split_kgrad_wins(const ssconv_rulebook* rb, int cin, int cout) {
   if (rb->n_pairs < 6 * (rb->n_in + rb->n_out)) return false;
   const KgradPlan r = kgrad_plan(rb, SSCONV_F32, cin, cout);
-  const KgradTile t = kgrad_tile(rb, 3, cin, cout);
+  const KgradTile t = kgrad_tile(rb, 3, cin, cout, false);
   const double pairs = (double)rb->n_pairs, partial = 8.0 * cin * cout / 4.5e6;
   const double r_units = std::max(rb->K, kgrad_f32_units_want(rb, cin, cout)), t_units = std::max(rb->K, t.units);
   const double r_tiles = r.mtiles * r.ntiles, t_tiles = t.mtiles * t.ntiles, B = r.wmb * r.wnb;
@@ -551,10 +551,10 @@ static bool use_kgrad_units(const ssconv_rulebook* rb, ssconv_dtype dt, int cin,
 // Work units of the kernel gradient: slices of about equal length, on the tile kernel (and the bf16 one in
 // columns, override 12) launched in the order of the rows, on the fp32 ring kernel enough wavefront tasks for one round of
 // the wavefront slots.
-static KgradUnits plan_units(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout, bool tiles) {
+static KgradUnits plan_units(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout, bool tiles, bool whole) {
   if (dt == SSCONV_F32 && !tiles)
     return kgrad_units(rb, kgrad_f32_units_want(rb, cin, cout), kKgradMaxUnitsF32);
-  return kgrad_units(rb, kgrad_tile(rb, dt == SSCONV_F32 ? 3 : 1, cin, cout).units, kKgradMaxUnits);
+  return kgrad_units(rb, kgrad_tile(rb, dt == SSCONV_F32 ? 3 : 1, cin, cout, whole).units, kKgradMaxUnits);
 }
 
 int bwd_rows(const void* feats, const void* grad_out, ssconv_dtype dt, int cin, int cout, const ssconv_rulebook* rb,
@@ -601,13 +601,14 @@ static auto feats_path(const ssconv_rulebook* rb, int cin, int cout) {
   return split && t_split < t_plain ? BwdLayout::kSplit : BwdLayout::kPlain;
 }
 
-BwdLayout bwd_layout(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout) {
+BwdLayout bwd_layout(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout, bool whole) {
   BwdLayout L;
+  L.whole = whole;
   const size_t K = rb->K, sz = dtype_bytes(dt);
   size_t nparts;  // fp32 partial tiles of cout x cin
   L.tiles = use_kgrad_tiles(rb, dt, cin, cout);
   if (L.tiles || use_kgrad_units(rb, dt, cin, cout)) {
-    L.units = plan_units(rb, dt, cin, cout, L.tiles);
+    L.units = plan_units(rb, dt, cin, cout, L.tiles, whole);
     nparts = (size_t)L.units.nunits;
   } else {
     L.nsplit = kgrad_supported(dt, cin, cout) ? kgrad_plan(rb, dt, cin, cout).nsplit : dw_nsplit(rb);
@@ -723,8 +724,8 @@ int conv_backward_dw(const void* feats, const void* grad_out, ssconv_dtype dt, i
     const KgradUnits& units = L.units;
     if (rows.parts) {
       const SplitFlags flags{rows.parts == 3 ? (int*)(ws + L.flags) : nullptr};
-      SSC_TRY(kgrad_tiles(rows.grad_out, rows.feats, rows.parts, cin, cout, rb, kgrad_tile(rb, rows.parts, cin, cout),
-                          units, kgrad_order(units), flags, part, st));
+      SSC_TRY(kgrad_tiles(rows.grad_out, rows.feats, rows.parts, cin, cout, rb,
+                          kgrad_tile(rb, rows.parts, cin, cout, L.whole), units, kgrad_order(units), flags, part, st));
       if (rows.parts == 3)  // the same units on the fp32 matrix cores
         SSC_TRY(kgrad_f32(grad_out, feats, cin, cout, rb, units, part, st,
                           {flags.grad_out(), flags.feats(), flags.kgrad()}));

@@ -14,6 +14,7 @@ struct BwdLayout {
                       // (without copies it starts at `rows`)
   int nsplit = 1;
   bool tiles = false;       // the kernel gradient on the tile kernel
+  bool whole = false;       // ... with its largest tiles too (kgrad_tile)
   bool split_rows = false;  // it reads split rows
   KgradUnits units;         // its work units (none: per-offset splits)
   enum { kPair, kSplit, kBf16, kPlain } feats = kPlain;  // the kernel of the feature gradient
@@ -46,7 +47,7 @@ int conv_forward(const void* feats, ssconv_dtype dt, int cin, const ssconv_ruleb
 // y = the convolution, z = Norm(y) over the fields f of the output channels (z may alias y).
 int conv_forward_norm(const void* feats, ssconv_dtype dt, int cin, const ssconv_rulebook* rb, const void* W, int cout,
                       const FieldTab& f, double eps, void* y, void* z, hipStream_t st);
-BwdLayout bwd_layout(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout);
+BwdLayout bwd_layout(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout, bool whole);
 int conv_backward_feats(const void* grad_out, ssconv_dtype dt, int cin, int cout, const ssconv_rulebook* rb,
                         const void* W, void* grad_feats, char* ws, const BwdLayout& L, const BwdRows& rows,
                         hipStream_t st);

@@ -41,7 +41,7 @@ constexpr int kPairBlock = 512;  // pair indices staged per block, double-buffer
 template <int P, int WM, int WN>
 struct KT {
   static constexpr int S = P == 1 ? 4 : 3;              // LDS stages
-  static constexpr int Q = P * (WM + WN);               // quads per stage: grad_out's, then feats'
+  static constexpr int Q = (P * (WM + WN) + 1) / 2 * 2;  // quads per stage: grad_out's, then feats' (an odd one out is never read)
   static constexpr int STAGE = 2048 * Q;
   static constexpr int L = Q / 2;                       // DMAs per wavefront per chunk: half of every other quad
   static constexpr int SMEM = S * STAGE + 2 * kPairBlock * 8;
@@ -282,11 +282,13 @@ int launch(const KgradRows& G, const KgradRows& F, int cin, int cout, const ssco
 // Split rows: four rounds, since their gathers miss the L2 more (an XCD runs all offsets of a stretch of rows
 // together: 36k sites, 5x5x5, 104 -> 104, as many slices of every list: 2 slices 780 us, 4 661, 8 596, 12 617;
 // in equal pieces the training step of that layer 1634 -> 1594).
-KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout) {
-  static const int shapes[][2] = {{2, 2}, {2, 4}, {4, 2}, {4, 4}, {7, 7}};
+// `whole` (bf16): tiles of 256 x 224 and 256 x 256 as well, which hold the kernel of a residual block of 208 channels and
+// its 48 gates at once; in 128 x 128 tiles every row is gathered twice (103.7k sites, 1.93M pairs, 208 -> 256: 414 us).
+KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout, bool whole) {
+  static const int shapes[][2] = {{2, 2}, {2, 4}, {4, 2}, {4, 4}, {7, 7}, {8, 7}, {8, 8}};
   KgradTile best{};
   double best_cost = 0.0;
-  for (int i = 0; i < (parts == 1 ? 5 : 4); ++i) {
+  for (int i = 0; i < (parts == 1 ? (whole ? 7 : 5) : 4); ++i) {
     KgradTile t;
     t.wm = shapes[i][0];
     t.wn = shapes[i][1];
@@ -308,6 +310,8 @@ int kgrad_tiles(const KgradRows& G, const KgradRows& F, int parts, int cin, int 
   if (units.nunits == 0) return SSCONV_OK;
 #define SSK_GO(P_, M_, N_) return launch<P_, M_, N_>(G, F, cin, cout, rb, t, units, order, flags, part, st)
   if (parts == 1) {
+    if (t.wm == 8 && t.wn == 8) SSK_GO(1, 8, 8);
+    if (t.wm == 8) SSK_GO(1, 8, 7);
     if (t.wm == 7) SSK_GO(1, 7, 7);
     if (t.wm == 4 && t.wn == 4) SSK_GO(1, 4, 4);
     if (t.wm == 4) SSK_GO(1, 4, 2);

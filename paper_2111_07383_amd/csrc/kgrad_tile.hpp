@@ -18,7 +18,7 @@ struct KgradRows {
 struct KgradTile {
   int wm, wn, mtiles, ntiles, units;
 };
-KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout);
+KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout, bool whole);
 
 // part[u][o][i] (fp32) = sum over unit u's slice of R_s of grad_out[x][o] feats[y][i].  flags (split rows): where a
 // word of the rows or of the sums is set afterwards, part is not valid.

@@ -74,6 +74,7 @@ def random_sites(rng, n, grid, batch=1):
 CONV = {
     "f104_k3_f32": (((0, 16), (1, 16), (2, 8)), 3, torch.float32, 900, 12),
     "f208_k3_bf16": (((0, 32), (1, 32), (2, 16)), 3, torch.bfloat16, 1500, 14),
+    "f232_k3_bf16": (((0, 220), (1, 4)), 3, torch.bfloat16, 300, 8),    # the kernel gradient's largest tile
     "ragged_k5_bf16": (((0, 13), (1, 11), (2, 5)), 5, torch.bfloat16, 400, 9),
     "tiny_k3_f32": (((0, 2), (1, 2)), 3, torch.float32, 60, 6),
     "one_site_f32": (((0, 4), (1, 1)), 3, torch.float32, 1, 4),
@@ -104,7 +105,7 @@ def test_backward_packed(name, norm):
     p = P.pack(f, dev(x, dtype))
     kw = dict(norm=True, gain=dev(gain), eps=1e-5) if norm else {}
     gf, gc = P.backward_packed(p, dev(g, dtype), rb, W, desc, basis, **kw)
-    # the same bits as the rows that the checkpoint stands for
+    # the same bits as the rows that the checkpoint stands for (few pairs: as many work units on either tile)
     rows = P.site_norm_forward(f, p, dev(gain), 1e-5, dtype=dtype) if norm else P.unpack(p, dtype)
     rf, rc = P.backward(rows, dev(g, dtype), rb, W, desc, basis)
     assert torch.equal(gf, rf) and torch.equal(gc, rc)
