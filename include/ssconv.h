@@ -355,7 +355,7 @@ int ssconv_site_norm_backward(const ssconv_fields* fields /*host*/, const ssconv
  * neither): checkpoints (ssconv_pack) of y (with the gates as the last entry) and
  * of h_out.  h_out may be h's buffer.
  *
- * Backward: from y and h_out (as rows or as checkpoints), dh [n, C] = gradient of
+ * Backward: from y and h_out (both as rows or both as checkpoints), dh [n, C] = gradient of
  * h_out and dx [n, C] = gradient of x_out (NULL where there was none; h_out may then
  * be NULL): dy [n, C + G], dh_in [n, C] = gradient of h, and dgain_post, dscale,
  * dgain_next (fp32, each NULL to skip; dgain_next NULL without dx), summed over the

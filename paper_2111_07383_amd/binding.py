@@ -614,7 +614,7 @@ def residual_backward(fields: FieldList, y: Union[torch.Tensor, Packed],
                       gain_post: Optional[torch.Tensor] = None, gain_next: Optional[torch.Tensor] = None,
                       eps: float = NORM_EPS, workspace: Optional[torch.Tensor] = None, stream=None):
     """ssconv_residual_backward: (dy, gradient of h, dscale, dgain_post, dgain_next) from the gradients dh of h_out and
-    dx of x_out (None without the next norm; h_out may then be None); y and h_out as rows or as checkpoints.  The
+    dx of x_out (None without the next norm; h_out may then be None); y and h_out both as rows or both as checkpoints.  The
     gradient of a parameter that is None is None."""
     t, dev = _table(fields), torch.cuda.current_device()
     full = t.full
@@ -625,6 +625,8 @@ def residual_backward(fields: FieldList, y: Union[torch.Tensor, Packed],
         _check(dx, "dx", dev, dtype, (n, t.C))
         if h_out is None:
             raise ValueError("dx needs h_out")
+        if isinstance(y, Packed) != isinstance(h_out, Packed):
+            raise ValueError("y and h_out are rows, or both are checkpoints")
         hr = _check_rows(h_out, "h_out", dev, t, n, dtype)
     elif gain_next is not None:
         raise ValueError("gain_next without dx")

@@ -259,6 +259,8 @@ extern "C" int ssconv_residual_backward(const ssconv_fields* fields, const sscon
   SSC_TRY(check_site_eps(eps));
   if (n > 0 && (!y || !y->data || !dh || !dy || !dh_in)) return fail(SSCONV_E_INVALID, "NULL feature buffer");
   if (n > 0 && dx && (!h_out || !h_out->data)) return fail(SSCONV_E_INVALID, "dx needs h_out");
+  if (n > 0 && dx && !y->exps != !h_out->exps)
+    return fail(SSCONV_E_INVALID, "y and h_out are rows, or both are checkpoints");
   if (n > 0 && !dx && (gain_next || dgain_next)) return fail(SSCONV_E_INVALID, "a next norm without dx");
   const int S = ty.ch0[ty.n], C = ty.C, stride = S + 2 * C;
   float* part = nullptr;

@@ -48,8 +48,8 @@ inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 // per SIMD.  All loop over the rows, so a grid of more would run in rounds of which the last is part empty (backward of
 // a 208-channel tail: 1024 workgroups of which 768 fit 235 us).
 constexpr int norm_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 4 : rag ? 5 : 8; }
-constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag || L == 64 ? 5 : 8; }
-constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag ? 4 : 6; }
+constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag || L == 64 ? 5 : 6; }
+constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag ? 4 : L == 64 ? 5 : 6; }
 constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : L == 64 ? 3 : 4; }
 inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
   const int64_t rows = site_rows(t);

@@ -6,31 +6,31 @@
 namespace ssconv {
 namespace {
 
-template <typename T, int L, int K, bool RAG>
+template <typename T, int L, int K, bool RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void norm_fwd_kernel(SiteTab t, NormArgs a) {
   using R = Row<L, K, RAG>;
   R w;
   w.init(t, t.n);
   const int C = t.ch0[t.n], B = t.b0[t.n];
   f8 g[K];
-  w.params(a.gain, g, t.n);
+  w.params(a.gain, g, t.f0[t.n]);
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
   for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
     f8 x[K];
-    float r[K];
+    float r[K], xs[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = w.template load_rows<T>(a.x, r0, row, C, B, k, w.start[k], w.blk[k]);
+    for (int k = 0; k < K; ++k) x[k] = w.template load_rows<T, PK>(a.x, r0, row, C, B, k, w.start[k], w.blk[k], xs[k]);
     if (a.q) w.pack(x, a.q + r0 * C, a.exps + r0 * B, row, C, B, t.n, on);
-    w.norm(x, r, a.eps);
+    w.norm(x, xs, r, a.eps);
 #pragma unroll
     for (int k = 0; k < K; ++k)
       if (on) w.template store<T>((T*)a.out + r0 * C, row, C, k, x[k] * g[k]);
   }
 }
 
-template <typename T, int L, int K, bool RAG>
+template <typename T, int L, int K, bool RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_kernel(SiteTab t, NormArgs a) {
   extern __shared__ float lds[];
   using R = Row<L, K, RAG>;
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_
   w.init(t, t.n);
   const int C = t.ch0[t.n], B = t.b0[t.n];
   f8 g[K], acc[K];
-  w.params(a.gain, g, t.n);
+  w.params(a.gain, g, t.f0[t.n]);
 #pragma unroll
   for (int k = 0; k < K; ++k) acc[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
@@ -46,18 +46,22 @@ __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
     f8 x[K], d[K], res[K];
-    float r[K];
+    float r[K], xs[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k] = w.template load_rows<T>(a.x, r0, row, C, B, k, w.start[k], w.blk[k]);
+      x[k] = w.template load_rows<T, PK>(a.x, r0, row, C, B, k, w.start[k], w.blk[k], xs[k]);
       d[k] = w.template load<T>((const T*)a.dy + r0 * C, row, C, k, w.start[k]);
       res[k] = f8{0, 0, 0, 0, 0, 0, 0, 0};
       if (a.dres) res[k] = w.template load<T>((const T*)a.dres + r0 * C, row, C, k, w.start[k]);
     }
-    w.norm(x, r, a.eps);
+    if (a.n - r0 < R::R)  // a row read a second time adds nothing
+#pragma unroll
+      for (int k = 0; k < K; ++k) d[k] = on ? d[k] : f8{0, 0, 0, 0, 0, 0, 0, 0};
+    w.norm(x, xs, r, a.eps);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (on) acc[k] += d[k] * x[k];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[k][c] = fmaf(d[k][c], x[k][c], acc[k][c]);
       d[k] *= g[k];
     }
     w.norm_back(x, r, d);
@@ -96,8 +100,11 @@ __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void unpack_ke
   for (int64_t r0 = first_row<R::R>(); r0 < n; r0 += step) {
     if (w.sub < n - r0)
 #pragma unroll
-      for (int k = 0; k < K; ++k)
-        w.template store<T>(x + r0 * C, w.sub, C, k, w.load_packed(q + r0 * C, exps + r0 * B, w.sub, C, B, k, w.start[k], w.blk[k]));
+      for (int k = 0; k < K; ++k) {
+        float s;
+        const f8 v = w.load_packed(q + r0 * C, exps + r0 * B, w.sub, C, B, k, w.start[k], w.blk[k], s);
+        w.template store<T>(x + r0 * C, w.sub, C, k, v * s);
+      }
   }
 }
 
@@ -111,7 +118,10 @@ int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStr
     return (int)SSCONV_OK;
   };
 #define SSK_GO(L_, K_, R_) \
-  return dt == SSCONV_F32 ? go(norm_fwd_kernel<float, L_, K_, R_>) : go(norm_fwd_kernel<uint16_t, L_, K_, R_>)
+  return a.x.exps ? dt == SSCONV_F32 ? go(norm_fwd_kernel<float, L_, K_, R_, true>)       \
+                                     : go(norm_fwd_kernel<uint16_t, L_, K_, R_, true>)    \
+         : dt == SSCONV_F32 ? go(norm_fwd_kernel<float, L_, K_, R_, false>)                \
+                            : go(norm_fwd_kernel<uint16_t, L_, K_, R_, false>)
   SSK_SITE_DISPATCH(t, SSK_GO);
 #undef SSK_GO
 }
@@ -125,7 +135,10 @@ int launch_norm_bwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStr
     return (int)SSCONV_OK;
   };
 #define SSK_GO(L_, K_, R_) \
-  return dt == SSCONV_F32 ? go(norm_bwd_kernel<float, L_, K_, R_>) : go(norm_bwd_kernel<uint16_t, L_, K_, R_>)
+  return a.x.exps ? dt == SSCONV_F32 ? go(norm_bwd_kernel<float, L_, K_, R_, true>)       \
+                                     : go(norm_bwd_kernel<uint16_t, L_, K_, R_, true>)    \
+         : dt == SSCONV_F32 ? go(norm_bwd_kernel<float, L_, K_, R_, false>)                \
+                            : go(norm_bwd_kernel<uint16_t, L_, K_, R_, false>)
   SSK_SITE_DISPATCH(t, SSK_GO);
 #undef SSK_GO
 }

@@ -124,9 +124,10 @@ struct Row {
       scalar[k] = false;
     }
 #pragma unroll
-    for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {  // those past the last hold no chunk
+    for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {
+      if (en >= entries) break;
       const int t0 = t.t0[en], t1 = t.t0[en + 1], ch0 = t.ch0[en], w = t.ch0[en + 1] - ch0;
-      any_scalar |= en < entries && t.l[en] == 0;
+      any_scalar |= t.l[en] == 0;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int c = i + k * L, j = c - t0, at = 8 * j;
@@ -193,10 +194,12 @@ struct Row {
     return v;
   }
 
-  // The same of a checkpoint of C channels and B blocks: the int8 values and the exponent bytes.
-  __device__ __forceinline__ f8 load_packed(const void* p, const uint8_t* b, int r, int C, int B, int k, int s,
-                                            int bl) const {
+  // The same of a checkpoint of C channels and B blocks: the int8 values and the exponent bytes.  The values are scale
+  // times what is returned; a chunk of two blocks (ragged) has them multiplied here.
+  __device__ __forceinline__ f8 load_packed(const void* p, const uint8_t* b, int r, int C, int B, int k, int s, int bl,
+                                            float& scale) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    scale = 1.f;
     if (RAG && hi[k] == 0) return v;
     const int8_t* at = (const int8_t*)p + (uint32_t)(__umul24(r, C) + s);
     u2 q = {0, 0};
@@ -208,22 +211,29 @@ struct Row {
         if (c < hi[k]) q[c / 4] |= (uint32_t)(uint8_t)at[c] << (8 * (c & 3));
     }
     const float x = pack_scale(b[(uint32_t)(__umul24(r, B) + bl)]);
-    const float x_lo = RAG && lo[k] > 0 ? pack_scale(b[(uint32_t)(__umul24(r, B) + blk_lo[k])]) : x;
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
-      v[c] = (float)(int8_t)(q[c / 4] >> (8 * (c & 3))) * (RAG && c < lo[k] ? x_lo : x);
-    if (RAG && hi[k] < 8)  // 0 * NaN
+    for (int c = 0; c < 8; ++c) v[c] = (float)(int8_t)(q[c / 4] >> (8 * (c & 3)));
+    if (!RAG) {
+      scale = x;
+      return v;
+    }
+    const float x_lo = lo[k] > 0 ? pack_scale(b[(uint32_t)(__umul24(r, B) + blk_lo[k])]) : x;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] *= c < lo[k] ? x_lo : x;
+    if (hi[k] < 8)  // 0 * NaN
 #pragma unroll
       for (int c = 1; c < 8; ++c)
         if (c >= hi[k]) v[c] = 0.f;
     return v;
   }
 
-  // Rows, or a checkpoint of them, from row r0 on.
-  template <typename T>
-  __device__ __forceinline__ f8 load_rows(const ssconv_rows& x, int64_t r0, int r, int C, int B, int k, int s,
-                                          int bl) const {
-    if (x.exps) return load_packed((const int8_t*)x.data + r0 * C, x.exps + r0 * B, r, C, B, k, s, bl);
+  // Rows, or (PK) a checkpoint of them, from row r0 on.  Which it is belongs to the kernel: with a branch here every
+  // matrix would be waited for before the next is asked for.
+  template <typename T, bool PK>
+  __device__ __forceinline__ f8 load_rows(const ssconv_rows& x, int64_t r0, int r, int C, int B, int k, int s, int bl,
+                                          float& scale) const {
+    if constexpr (PK) return load_packed((const int8_t*)x.data + r0 * C, x.exps + r0 * B, r, C, B, k, s, bl, scale);
+    scale = 1.f;
     return load<T>((const T*)x.data + r0 * C, r, C, k, s);
   }
 
@@ -345,19 +355,26 @@ struct Row {
     return fabsf(q) < 3e38f ? r : q;
   }
 
-  // xhat in place of x; r = 1 / sqrt(v + eps).
-  __device__ __forceinline__ void norm(f8 (&x)[K], float (&r)[K], float eps) const {
+  // xhat in place of x, whose values are scale times x; r = 1 / sqrt(v + eps).
+  __device__ __forceinline__ void norm(f8 (&x)[K], const float (&scale)[K], float (&r)[K], float eps) const {
+    float mu[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) mu[k] = 0.f;
     if (any_scalar) {
       float s[1][K];
 #pragma unroll
-      for (int k = 0; k < K; ++k) s[0][k] = of(x[k], k);
+      for (int k = 0; k < K; ++k) s[0][k] = of(x[k], k) * scale[k];
       sums(s);
 #pragma unroll
-      for (int k = 0; k < K; ++k) x[k] -= scalar[k] ? over_m(s[0][k], k) : 0.f;
+      for (int k = 0; k < K; ++k) mu[k] = scalar[k] ? over_m(s[0][k], k) : 0.f;
     }
     float s[1][K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) s[0][k] = dot(x[k], x[k], k);
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[k][c] = fmaf(x[k][c], scale[k], -mu[k]);
+      s[0][k] = dot(x[k], x[k], k);
+    }
     sums(s);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -365,8 +382,14 @@ struct Row {
       x[k] *= r[k];
     }
   }
+  __device__ __forceinline__ void norm(f8 (&x)[K], float (&r)[K], float eps) const {
+    float one[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) one[k] = 1.f;
+    norm(x, one, r, eps);
+  }
 
-  // Gradient behind a norm in place of t = gain * dy, from xhat and r.
+  // Gradient behind a norm in place of t = gain * dy, from xhat and r: r t - r mean(t) - xhat r sum(t xhat) / m.
   __device__ __forceinline__ void norm_back(const f8 (&xhat)[K], const float (&r)[K], f8 (&t)[K]) const {
     float s[2][K];
 #pragma unroll
@@ -377,19 +400,20 @@ struct Row {
     sums(s);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const float a = scalar[k] ? s[0][k] * rm[k] : 0.f, b = s[1][k] * rm[k];
+      const float rr = r[k] * rm[k], a = scalar[k] ? s[0][k] * rr : 0.f, b = s[1][k] * rr;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) t[k][c] = r[k] * (t[k][c] - a - xhat[k][c] * b);
+      for (int c = 0; c < 8; ++c) t[k][c] = fmaf(t[k][c], r[k], fmaf(-xhat[k][c], b, -a));
     }
   }
 
-  // A parameter per field as one per channel of the chunks (ones without it).
-  __device__ __forceinline__ void params(const float* p, f8 (&v)[K], int entries) const {
+  // A parameter of `fields` values, one per field, as one per channel of the chunks; ones without it.  Chunks past its
+  // fields (the gates of a parameter of the fields) get its last value: looking at them here would wait for the loads,
+  // which the first row's overlap.
+  __device__ __forceinline__ void params(const float* p, f8 (&v)[K], int fields) const {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        v[k][c] = p && e[k] < entries && c < hi[k] ? p[f0[k] + field(k, c)] : 1.f;
+      for (int c = 0; c < 8; ++c) v[k][c] = p ? p[min(f0[k] + field(k, c), fields - 1)] : 1.f;
   }
 
   // The checkpoint of row r: int8 values at q, exponent bytes at b; of the chunks of the first `entries` entries.
@@ -469,50 +493,75 @@ template <int L, int K, bool RAG>
 struct Gates {
   static constexpr int Q = Row<L, K, RAG>::Q;
   int c0[Q], d[Q], at[Q];  // d = 0: none; at: the gate's own channel
+  int most;                // components of the largest order (uniform)
 
-  __device__ __forceinline__ void init(const SiteTab& t, int i) {
+  // d[q] for a comparison made where it stands: hoisted out of the loop over the rows, the comparisons' masks take more
+  // scalar registers than there are (60 v_readlane a row).
+  __device__ __forceinline__ int comps(int q) const {
+    int v = d[q];
+    asm volatile("" : "+v"(v));
+    return v;
+  }
+
+  // scale (optional): v[q] = the parameter of the field that a gate opens.
+  __device__ __forceinline__ void init(const SiteTab& t, int i, const float* p, float (&v)[Q]) {
+    int f0[Q];
+    most = 0;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const int g = i + q * L;
-      c0[q] = d[q] = 0;
-      at[q] = t.C + g;
+      c0[q] = d[q] = f0[q] = 0;
+      at[q] = t.C + i + q * L;
+      v[q] = 1.f;
+    }
 #pragma unroll
-      for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {
-        const int f = g - t.gate0[en], dd = 2 * t.l[en] + 1;
-        const bool in = en < t.n_regular && t.l[en] > 0 && f >= 0 && f < t.mult[en];
+    for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {
+      if (en >= t.n_regular) break;
+      const int dd = 2 * t.l[en] + 1;
+      most = max(most, dd);
+      if (dd == 1) continue;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int f = i + q * L - t.gate0[en];
+        const bool in = f >= 0 && f < t.mult[en];
         c0[q] = in ? t.ch0[en] + f * dd : c0[q];
+        f0[q] = in ? t.f0[en] + f : f0[q];
         d[q] = in ? dd : d[q];
       }
     }
+    if (p)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) v[q] = p[f0[q]];
   }
 
-  // buf[channel]: from the gates' inputs in their channels, their sigmoids in all components of what they gate.
-  __device__ __forceinline__ void open(float* buf, float (&s)[Q]) const {
+  // buf[channel], of a row that ends at `end`: from the gates' inputs in their channels, their sigmoids in all components of what they gate.
+  __device__ __forceinline__ void open(float* buf, int end, float (&s)[Q]) const {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) s[q] = d[q] ? buf[at[q]] : 0.f;
+    for (int q = 0; q < Q; ++q) s[q] = buf[min(at[q], end)];
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      if (d[q] == 0) continue;
+      const int n = comps(q);
       s[q] = sigmoid_of(s[q]);
+      if (n == 0) continue;
       float* b = buf + c0[q];
       b[0] = b[1] = b[2] = s[q];
-      if (d[q] > 3) b[3] = b[4] = s[q];
-      if (d[q] > 5) b[5] = b[6] = s[q];
-      if (d[q] > 7) b[7] = b[8] = s[q];
+      if (n > 3) b[3] = b[4] = s[q];
+      if (most > 5 && n > 5) b[5] = b[6] = s[q];
+      if (most > 7 && n > 7) b[7] = b[8] = s[q];
     }
   }
 
-  // From the products dg * u in the components, the gates' gradients in their channels.
-  __device__ __forceinline__ void close(float* buf, const float (&s)[Q]) const {
+  // From the products dh * u in the components, the gates' gradients in their channels.
+  __device__ __forceinline__ void close(float* buf, const float (&s)[Q], const float (&scale)[Q]) const {
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      if (d[q] == 0) continue;
+      const int n = comps(q);
+      if (n == 0) continue;
       const float* b = buf + c0[q];
       float v = (b[0] + b[1]) + b[2];
-      if (d[q] > 3) v += b[3] + b[4];
-      if (d[q] > 5) v += b[5] + b[6];
-      if (d[q] > 7) v += b[7] + b[8];
-      buf[at[q]] = v * (s[q] * (1.f - s[q]));
+      if (n > 3) v += b[3] + b[4];
+      if (most > 5 && n > 5) v += b[5] + b[6];
+      if (most > 7 && n > 7) v += b[7] + b[8];
+      buf[at[q]] = v * (scale[q] * (s[q] * (1.f - s[q])));
     }
   }
 };

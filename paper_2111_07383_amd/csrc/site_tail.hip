@@ -8,7 +8,7 @@
 namespace ssconv {
 namespace {
 
-constexpr f8 kZero = {0, 0, 0, 0, 0, 0, 0, 0};
+constexpr f8 kZero = {0, 0, 0, 0, 0, 0, 0, 0}, kOne = {1, 1, 1, 1, 1, 1, 1, 1};
 
 template <typename T, int L, int K, bool RAG>
 __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_kernel(SiteTab t, TailArgs a, int lds_row) {
@@ -17,19 +17,23 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
   R w;
   Gates<L, K, RAG> gates;
   w.init(t, t.n);
-  gates.init(t, w.i);
+  float unused[R::Q];
+  gates.init(t, w.i, nullptr, unused);
   const int C = t.C, S = t.ch0[t.n], By = t.b0[t.n], Bh = t.b0[t.n_regular], G = t.G;
   float* buf = lds + ((threadIdx.x >> 6) * R::R + w.sub) * lds_row;
   f8 gp[K], sc[K], gn[K];
-  w.params(a.gain_post, gp, t.n);
-  w.params(a.scale, sc, t.n_regular);
-  w.params(a.gain_next, gn, t.n_regular);
+  w.params(a.gain_post, gp, t.f0[t.n]);
+  w.params(a.scale, sc, t.f0[t.n_regular]);
+  w.params(a.gain_next, gn, t.f0[t.n_regular]);
   bool main[K];  // a chunk of the fields, not of the gates
   int at[K];     // its place in a matrix without the gates
+  float least[K];  // a gated value counts above this: relu of the scalars, everything else
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
     at[k] = main[k] ? w.start[k] : 0;
+    least[k] = w.scalar[k] ? 0.f : -__builtin_inff();
+    if (G && main[k] && w.scalar[k]) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
   }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
   for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
@@ -50,16 +54,15 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
       for (int k = 0; k < K; ++k)
         if (w.hi[k] > 0 && !main[k]) lds_put(w, k, buf, y[k] * gp[k]);
       wave_lds_fence();
-      gates.open(buf, sig);
+      gates.open(buf, S, sig);
       wave_lds_fence();
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const f8 f = G ? lds_get(w, k, buf) : kZero;
+      const f8 f = G ? lds_get(w, k, buf) : kOne;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        const float u = y[k][c] * gp[k][c];
-        const float g = w.scalar[k] ? (u <= 0.f ? 0.f : u) : f[c] * u;  // NaN stays
+        const float u = y[k][c] * gp[k][c], g = u <= least[k] ? 0.f : f[c] * u;  // NaN stays
         h[k][c] = fmaf(sc[k][c], g, h[k][c]);
       }
       h[k] = round8<T>(h[k]);
@@ -76,21 +79,25 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
   }
 }
 
-// The parameters and their gradients' sums take 48 of a lane's registers.
-template <typename T, int L, int K, bool RAG>
+// With e = dh times the gate's factor (1 or 0 for a scalar; a gate channel's own gradient there), the gradients of both
+// parameters of the block's output are the same sum over the rows: dscale = gain_post sum(e yhat),
+// dgain_post = scale sum(e yhat); and what goes on behind the norm is scale gain_post e.  The components of a field
+// share both parameters, so its gate's lane multiplies their sum of dh u by the scale.
+template <typename T, int L, int K, bool RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_kernel(SiteTab t, TailArgs a, int lds_row) {
   extern __shared__ __attribute__((aligned(32))) float lds[];
   using R = Row<L, K, RAG>;
   R w;
   Gates<L, K, RAG> gates;
   w.init(t, t.n);
-  gates.init(t, w.i);
+  float gate_scale[R::Q];
+  gates.init(t, w.i, a.scale, gate_scale);
   const int C = t.C, S = t.ch0[t.n], By = t.b0[t.n], Bh = t.b0[t.n_regular], G = t.G;
   float* buf = lds + ((threadIdx.x >> 6) * R::R + w.sub) * lds_row;
-  f8 gp[K], sc[K], gn[K], acc_p[K], acc_s[K], acc_n[K];
-  w.params(a.gain_post, gp, t.n);
-  w.params(a.scale, sc, t.n_regular);
-  w.params(a.gain_next, gn, t.n_regular);
+  f8 gp[K], sc[K], gn[K], acc[K], acc_n[K];
+  w.params(a.gain_post, gp, t.f0[t.n]);
+  w.params(a.scale, sc, t.f0[t.n_regular]);
+  w.params(a.gain_next, gn, t.f0[t.n_regular]);
   bool main[K];
   int at[K], blk[K];
 #pragma unroll
@@ -98,91 +105,95 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
     main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
     at[k] = main[k] ? w.start[k] : 0;
     blk[k] = main[k] ? w.blk[k] : 0;
-    acc_p[k] = acc_s[k] = acc_n[k] = kZero;
+    sc[k] = main[k] ? sc[k] * gp[k] : gp[k];
+    acc[k] = acc_n[k] = kZero;
+    if (G && main[k] && w.scalar[k]) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
   }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
   for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
-    f8 y[K], dh[K];
-    float r[K], sig[R::Q];
+    f8 y[K], e[K], h[K], dx[K];
+    float r[K], ys[K], hs[K], sig[R::Q];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      y[k] = w.template load_rows<T>(a.y, r0, row, S, By, k, w.start[k], w.blk[k]);
-      dh[k] = kZero;
-      if (!RAG || main[k]) dh[k] = w.template load<T>((const T*)a.dh + r0 * C, row, C, k, at[k]);
+      y[k] = w.template load_rows<T, PK>(a.y, r0, row, S, By, k, w.start[k], w.blk[k], ys[k]);
+      e[k] = h[k] = dx[k] = kZero;
+      hs[k] = 1.f;
+      if (RAG && !main[k]) continue;
+      e[k] = w.template load<T>((const T*)a.dh + r0 * C, row, C, k, at[k]);
+      if (!a.dx) continue;
+      dx[k] = w.template load<T>((const T*)a.dx + r0 * C, row, C, k, at[k]);
+      h[k] = w.template load_rows<T, PK>(a.h, r0, row, C, Bh, k, at[k], blk[k], hs[k]);
     }
+    const bool part = a.n - r0 < R::R;  // a row read a second time adds nothing to the parameters' gradients
+    if (part && !on)
+#pragma unroll
+      for (int k = 0; k < K; ++k) e[k] = dx[k] = kZero;
     if (a.dx) {
-      f8 h[K], dx[K];
+      w.norm(h, hs, r, a.eps);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        h[k] = dx[k] = kZero;
-        if (RAG && !main[k]) continue;
-        dx[k] = w.template load<T>((const T*)a.dx + r0 * C, row, C, k, at[k]);
-        h[k] = w.template load_rows<T>(a.h, r0, row, C, Bh, k, at[k], blk[k]);
-      }
-      w.norm(h, r, a.eps);
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (on) acc_n[k] += dx[k] * h[k];
+        for (int c = 0; c < 8; ++c) acc_n[k][c] = fmaf(dx[k][c], h[k][c], acc_n[k][c]);
         dx[k] *= gn[k];
       }
       w.norm_back(h, r, dx);
 #pragma unroll
-      for (int k = 0; k < K; ++k) dh[k] += dx[k];
+      for (int k = 0; k < K; ++k) e[k] += dx[k];
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (on && main[k]) w.template store<T>((T*)a.dh_in + r0 * C, row, C, k, dh[k]);
-    w.norm(y, r, a.eps);
+      if (on && main[k]) w.template store<T>((T*)a.dh_in + r0 * C, row, C, k, e[k]);
+    w.norm(y, ys, r, a.eps);
     if (G) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (w.hi[k] > 0 && !main[k]) lds_put(w, k, buf, y[k] * gp[k]);
       wave_lds_fence();
-      gates.open(buf, sig);
+      gates.open(buf, S, sig);
       wave_lds_fence();
     }
-    f8 du[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const f8 f = G ? lds_get(w, k, buf) : kZero;
-      f8 gated, prod;
+      const f8 f = G ? lds_get(w, k, buf) : kOne;
+      f8 prod;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const float u = y[k][c] * gp[k][c];
-        const float on_off = u > 0.f ? 1.f : 0.f, fc = w.scalar[k] ? on_off : f[c];
-        const float dg = sc[k][c] * dh[k][c];
-        gated[c] = dh[k][c] * (fc * u);
-        du[k][c] = dg * fc;
-        prod[c] = dg * u;
+        prod[c] = e[k][c] * u;
+        e[k][c] *= u > 0.f || !w.scalar[k] ? f[c] : 0.f;
       }
-      if (on) acc_s[k] += gated;
-      if (G && main[k]) lds_put(w, k, buf, prod);
+      if (G && main[k] && !w.scalar[k]) lds_put(w, k, buf, prod);
     }
     if (G) {
       wave_lds_fence();
-      gates.close(buf, sig);
+      gates.close(buf, sig, gate_scale);
       wave_lds_fence();
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (w.hi[k] > 0 && !main[k]) du[k] = lds_get(w, k, buf);
+        if (w.hi[k] > 0 && !main[k]) e[k] = lds_get(w, k, buf);
       wave_lds_fence();
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (on) acc_p[k] += du[k] * y[k];
-      du[k] *= gp[k];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[k][c] = fmaf(e[k][c], y[k][c], acc[k][c]);
+      e[k] *= sc[k];
     }
-    w.norm_back(y, r, du);
+    w.norm_back(y, r, e);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (on) w.template store<T>((T*)a.dy + r0 * S, row, S, k, du[k]);
+      if (on) w.template store<T>((T*)a.dy + r0 * S, row, S, k, e[k]);
   }
   if (a.part) {
     float* out = a.part + (int64_t)blockIdx.x * (S + 2 * C);
-    sum_rows<L, K, RAG>(w, acc_p, S, lds, out);
-    sum_rows<L, K, RAG>(w, acc_s, C, lds, out + S);
+    f8 s[K];
+    w.params(a.scale, s, t.f0[t.n_regular]);
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[k] = main[k] ? s[k] * acc[k] : acc[k], acc[k] *= gp[k];
+    sum_rows<L, K, RAG>(w, s, S, lds, out);
+    sum_rows<L, K, RAG>(w, acc, C, lds, out + S);
     sum_rows<L, K, RAG>(w, acc_n, C, lds, out + S + C);
   }
 }
@@ -214,7 +225,10 @@ int launch_tail_bwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStr
     return (int)SSCONV_OK;
   };
 #define SSK_GO(L_, K_, R_) \
-  return dt == SSCONV_F32 ? go(tail_bwd_kernel<float, L_, K_, R_>) : go(tail_bwd_kernel<uint16_t, L_, K_, R_>)
+  return a.y.exps ? dt == SSCONV_F32 ? go(tail_bwd_kernel<float, L_, K_, R_, true>)       \
+                                     : go(tail_bwd_kernel<uint16_t, L_, K_, R_, true>)    \
+         : dt == SSCONV_F32 ? go(tail_bwd_kernel<float, L_, K_, R_, false>)                \
+                            : go(tail_bwd_kernel<uint16_t, L_, K_, R_, false>)
   SSK_SITE_DISPATCH(t, SSK_GO);
 #undef SSK_GO
 }

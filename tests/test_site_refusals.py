@@ -96,6 +96,8 @@ def test_missing_buffers():
     refused(L.ssconv_residual_forward(fields(F), P, N, 0, 1, 1e-5, N, N, N, P, P, N, N, N, N, N))
     refused(L.ssconv_residual_forward(fields(F), P, P, 0, 1, 1e-5, N, N, N, P, P, P, N, N, N, N))
     refused(L.ssconv_residual_forward(fields(F), P, P, 0, 1, 1e-5, N, N, P, P, N, N, N, N, N, N))   # gain_next alone
+    for y, h in ((rows(4096, 4096), rows()), (rows(), rows(4096, 4096))):                       # one a checkpoint
+        refused(L.ssconv_residual_backward(fields(F), y, h, P, P, 0, 1, 1e-5, N, N, N, P, P, N, N, N, N, 0, N))
     refused(L.ssconv_residual_backward(fields(F), rows(), N, P, P, 0, 1, 1e-5, N, N, N, P, P, N, N, N, N, 0, N))
     refused(L.ssconv_residual_backward(fields(F), rows(), rows(), P, N, 0, 1, 1e-5, N, N, P, P, P, N, N, N, N, 0, N))
     refused(L.ssconv_residual_backward(fields(F), rows(), rows(), P, N, 0, 1, 1e-5, N, N, N, P, P, N, N, P, P, 1 << 30, N))
