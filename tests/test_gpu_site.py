@@ -496,3 +496,35 @@ def test_binding_refusals():
         P.site_norm_backward(f, x, x, ok, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         P.unpack(P.Packed(full, P.pack(f, x).q, P.pack(f, x).exps))
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes and 2^31 elements in one matrix: the last rows are those of a small call, and the rows in
+    front of them are not touched by it."""
+    f, tail = FIELDS["f208"], 5
+    full = os_.gate_fields(f)
+    n = (1 << 31) // 208 + 1000
+    rng = np.random.default_rng(21)
+    part = dev(values(rng, tail, 208, torch.bfloat16), torch.bfloat16)
+    yp = dev(values(rng, tail, 256, torch.bfloat16), torch.bfloat16)
+    assert n * 208 > 1 << 31 and n * 208 * 2 > 1 << 32
+    h = torch.zeros((n, 208), dtype=torch.bfloat16, device=DEV)
+    y = torch.zeros((n, 256), dtype=torch.bfloat16, device=DEV)
+    h[-tail:], y[-tail:] = part, yp
+    small = P.residual_forward(f, yp, part, eps=EPS, checkpoint=True)
+    ho, x, yk, hk = P.residual_forward(f, y, h, eps=EPS, checkpoint=True, out=h)
+    assert torch.equal(ho[-tail:], small[0]) and torch.equal(x[-tail:], small[1])
+    assert torch.equal(yk.q[-tail:], small[2].q) and torch.equal(hk.exps[-tail:], small[3].exps)
+    assert not bool(x[:-tail].any()) and not bool(yk.q[:-tail].any())
+    del x, y
+    dh = torch.zeros((n, 208), dtype=torch.bfloat16, device=DEV)
+    dh[-tail:] = part
+    one = torch.ones(count(f), device=DEV)
+    sb = P.residual_backward(f, small[2], small[3], part, part, one, None, one, EPS)
+    dy, dhi, ds, _, dn = P.residual_backward(f, yk, hk, dh, dh, one, None, one, EPS)
+    assert torch.equal(dy[-tail:], sb[0]) and torch.equal(dhi[-tail:], sb[1]) and not bool(dy[:-tail].any())
+    # 5 rows of up to 5 components: sums of at most 25 products in two orders, off by 24 u of their magnitudes (about 5)
+    assert torch.allclose(ds, sb[2], rtol=1e-5, atol=1e-5) and torch.allclose(dn, sb[4], rtol=1e-5, atol=1e-5)
+    del dy, dhi, dh
+    assert torch.equal(P.unpack(hk)[-tail:], P.unpack(small[3]))
+    assert torch.equal(P.site_norm_forward(f, hk, eps=EPS)[-tail:], P.site_norm_forward(f, small[3], eps=EPS))
