@@ -33,12 +33,15 @@ struct SiteTab {
 // gated: the gates of the fields of order > 0 as one more entry.
 int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t);
 
-// Lanes per row: the fewest that hold a row with one chunk each, or 64 with three.
+// Lanes per row: the fewest that hold a row with one chunk each, or 64 with two or three.  Twice as many leave half of a
+// wavefront idle (backward of a residual tail, bf16: 150k rows of 36 channels on 8 lanes 53 us, on 16 86; 100k of 104 on
+// 16 38, on 32 55).  More chunks a lane than a row needs cost more than idle lanes, and their sums go entry by entry (60k
+// rows of 480 channels and 96 gates with two chunks 198 us, with three 402).
 inline int site_lanes(const SiteTab& t) {
   const int c = t.t0[t.n];
-  return c <= 16 ? 16 : c <= 32 ? 32 : 64;
+  return c <= 8 ? 8 : c <= 16 ? 16 : c <= 32 ? 32 : 64;
 }
-inline bool site_wide(const SiteTab& t) { return t.t0[t.n] > 64; }
+inline int site_chunks(const SiteTab& t) { return t.t0[t.n] <= 64 ? 1 : t.t0[t.n] <= 128 ? 2 : 3; }
 // Floats of LDS per row of the residual tail: the row, and 8 that a chunk moved off it may read.
 inline int site_lds_row(const SiteTab& t) { return (t.ch0[t.n] + 8 + 7) / 8 * 8; }
 // Rows that a workgroup takes at a time.
@@ -46,15 +49,17 @@ inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 
 // Workgroups of a compute unit at a time, by a kernel's registers (their launch bounds); a workgroup is one wavefront
 // per SIMD.  All loop over the rows, so a grid of more would run in rounds of which the last is part empty (backward of
-// a 208-channel tail: 1024 workgroups of which 768 fit 235 us).
-constexpr int norm_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 4 : rag ? 5 : 8; }
-constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag || L == 64 ? 5 : 6; }
-constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : rag ? 4 : L == 64 ? 5 : 6; }
-constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : L == 64 ? 3 : 4; }
+// a 208-channel tail: 1024 workgroups of 144 registers, of which 768 fit, 235 us; the next version, 1024 of 128
+// registers, 127).  The norm's backward would hold 8; its partial sums then cost more (191.8k rows of 208 channels forward and
+// backward with 8 97 us, 6 94, 4 101).
+constexpr int norm_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 4 : K == 2 || rag ? 5 : 8; }
+constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
+constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }
+constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : K == 2 ? 2 : L == 64 ? 3 : 4; }
 inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
   const int64_t rows = site_rows(t);
   return (unsigned)std::min<int64_t>((n + rows - 1) / rows,
-                                     256 * per_cu(site_lanes(t), site_wide(t) ? 3 : 1, t.ragged != 0));
+                                     256 * per_cu(site_lanes(t), site_chunks(t), t.ragged != 0));
 }
 
 struct NormArgs {

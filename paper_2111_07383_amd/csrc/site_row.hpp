@@ -7,9 +7,9 @@
 // computed and stored twice, with the same bits.  Entries under 8 channels have one chunk of `hi` channels, moved
 // element by element.
 //
-// With K = 1 an entry is a run of lanes, and its sums are a segmented prefix sum (4 to 6 DPP additions, whatever the
-// number of entries) of which the run's last lane is read back; with K = 3 (rows over 64 chunks) they are butterflies
-// entry by entry.
+// With K = 1 an entry is a run of lanes, and its sums are a segmented prefix sum (3 to 6 DPP additions, whatever the
+// number of entries) of which the run's last lane is read back; with K = 2 or 3 (rows over 64 or 128 chunks) they are sums
+// over the wavefront entry by entry.
 #pragma once
 
 #include "site.hpp"
@@ -47,6 +47,17 @@ __device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_r
 template <int CTRL>
 __device__ __forceinline__ float dpp_or_0(float v) {  // the value of another lane, 0 where there is none
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over the wavefront, in a scalar register.
+__device__ __forceinline__ float wave_total(float v) {
+  v += dpp_or_0<0x111>(v);  // the lane 1, 2, 4, 8 before
+  v += dpp_or_0<0x112>(v);
+  v += dpp_or_0<0x114>(v);
+  v += dpp_or_0<0x118>(v);
+  v += dpp_or_0<0x142>(v);  // lane 15 of the 16 before
+  v += dpp_or_0<0x143>(v);  // lane 31
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 __device__ __forceinline__ float read_lane(float v, int addr) {
@@ -280,6 +291,9 @@ struct Row {
       for (int a = 0; a < N; ++a) s[a] = v[a][0];
       if constexpr (N == 1) {
 #define SSK_STEP(CTRL) "s_nop 1\n\tv_fmac_f32_dpp %0, %0, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
+        if constexpr (L == 8)
+          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4")
+              : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4));
         if constexpr (L == 16)
           asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
               : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
@@ -295,6 +309,9 @@ struct Row {
 #define SSK_STEP(CTRL)                                                                  \
   "s_nop 1\n\tv_fmac_f32_dpp %0, %0, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t" \
   "v_fmac_f32_dpp %1, %1, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
+        if constexpr (L == 8)
+          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4")
+              : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4));
         if constexpr (L == 16)
           asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
               : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
@@ -320,7 +337,7 @@ struct Row {
         SSK_STEP(0x111, m1)
         SSK_STEP(0x112, m2)
         SSK_STEP(0x114, m4)
-        SSK_STEP(0x118, m8)
+        if constexpr (L >= 16) { SSK_STEP(0x118, m8) }
         if constexpr (L >= 32) { SSK_STEP(0x142, m15) }
         if constexpr (L >= 64) { SSK_STEP(0x143, m31) }
 #undef SSK_STEP
@@ -335,10 +352,9 @@ struct Row {
           float s = 0.f;
 #pragma unroll
           for (int k = 0; k < K; ++k) s += e[k] == en ? v[a][k] : 0.f;
+          const float all = wave_total(s);
 #pragma unroll
-          for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-#pragma unroll
-          for (int k = 0; k < K; ++k) out[a][k] = e[k] == en ? s : out[a][k];
+          for (int k = 0; k < K; ++k) out[a][k] = e[k] == en ? all : out[a][k];
         }
 #pragma unroll
       for (int a = 0; a < N; ++a)
@@ -613,14 +629,18 @@ __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc
   do {                                                               \
     const int chunks_ = (t_).t0[(t_).n];                             \
     if ((t_).ragged) {                                               \
+      if (chunks_ <= 8) GO_(8, 1, true);                             \
       if (chunks_ <= 16) GO_(16, 1, true);                           \
       if (chunks_ <= 32) GO_(32, 1, true);                           \
       if (chunks_ <= 64) GO_(64, 1, true);                           \
+      if (chunks_ <= 128) GO_(64, 2, true);                          \
       GO_(64, 3, true);                                              \
     }                                                                \
+    if (chunks_ <= 8) GO_(8, 1, false);                              \
     if (chunks_ <= 16) GO_(16, 1, false);                            \
     if (chunks_ <= 32) GO_(32, 1, false);                            \
     if (chunks_ <= 64) GO_(64, 1, false);                            \
+    if (chunks_ <= 128) GO_(64, 2, false);                           \
     GO_(64, 3, false);                                               \
   } while (0)
 

@@ -33,15 +33,18 @@ FIELDS = {
     "ragged": ((0, 13), (1, 11), (2, 5)),
     "order4": ((4, 3), (0, 9), (3, 2), (0, 1)),
     "seven": ((0, 8), (1, 3), (0, 40), (2, 2), (1, 9), (3, 1), (4, 1)),
+    "f36": ((0, 4), (1, 4), (2, 4)),
+    "w52": ((0, 8), (1, 8), (2, 4)),                 # 52 + 12 gates: 64
     "w61": ((0, 33), (0, 28)),
     "w128": ((0, 40), (1, 10), (2, 8)),              # 110 + 18 gates: 128
     "w256": ((0, 128), (1, 24), (2, 4)),             # 220 + 28
     "w400": ((0, 100), (1, 50), (2, 30)),            # 400 + 80
     "w510": ((1, 127),),                             # 381 + 127
     "w900": ((0, 500), (1, 100), (2, 10)),           # 850 + 110
-    "w1024": ((0, 496), (1, 100), (2, 16), (0, 32)),  # 908 + 116: all of the 1024
+    "w1024": ((0, 496), (1, 100), (2, 16), (0, 32)),  # 908 + 116: all of the 1024, 129 chunks of 8
 }
-NORM_ONLY = {"eight": ((0, 3), (1, 2)) * 4, "all1024": ((0, 1024),), "vec1023": ((1, 341),)}
+NORM_ONLY = {"eight": ((0, 3), (1, 2)) * 4, "all1024": ((0, 1024),), "vec1023": ((1, 341),),
+             "odd1023": ((0, 129),) * 7 + ((0, 120),)}
 ROWS = [1, 3, 37]
 
 
