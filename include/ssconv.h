@@ -319,8 +319,8 @@ int ssconv_forward_norm(const void* feats, ssconv_dtype dtype, int cin, ssconv_r
  * the gradient that reaches x past the norm; dgain fp32 [fields] (NULL: skipped)
  * = sum over rows of dy * y / gain, in a fixed order (deterministic).  dx may be
  * dy's or dres's buffer.  workspace: device scratch of at least
- * ssconv_site_norm_workspace_size bytes, 256-byte aligned, needed where dgain is
- * given; calls that overlap in time need their own.
+ * ssconv_site_norm_workspace_size bytes (0 for a few rows), 256-byte aligned, needed
+ * where dgain is given; calls that overlap in time need their own.
  * n = 0: dgain becomes 0, nothing else is written.  Nothing is allocated and the
  * stream is not synchronised.  Feature buffers need the alignment of their
  * elements only; no buffers may overlap but those named here.

@@ -434,6 +434,11 @@ class Packed:
                       torch.empty((n, packed_blocks(t.fields)), dtype=torch.uint8, device=device))
 
 
+def _new_packed(t: _Table, n: int, like: torch.Tensor) -> Packed:
+    blocks = t.blocks or packed_blocks(t.fields)
+    return Packed(t.fields, like.new_empty((n, t.C), dtype=torch.int8), like.new_empty((n, blocks), dtype=torch.uint8))
+
+
 def _check(t: torch.Tensor, name: str, dev: int, dtype, shape):
     """A contiguous tensor of this type and shape on the current device."""
     if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
@@ -457,7 +462,7 @@ def _check_packed(p: Packed, name: str, dev: int, t: _Table, n: int):
     if p.fields is not t.fields and _table(p.fields).fields != t.fields:
         raise ValueError(f"{name} is a checkpoint of fields {tuple(p.fields)}, not {t.fields}")
     _check(p.q, name + ".q", dev, torch.int8, (n, t.C))
-    _check(p.exps, name + ".exps", dev, torch.uint8, (n, packed_blocks(t.fields) if t.blocks == 0 else t.blocks))
+    _check(p.exps, name + ".exps", dev, torch.uint8, (n, t.blocks or packed_blocks(t.fields)))
 
 
 def _check_rows(x, name: str, dev: int, t: _Table, n: int, dtype) -> Rows:
@@ -476,9 +481,9 @@ def _param(p: Optional[torch.Tensor], name: str, dev: int, t: _Table):
     return p.data_ptr()
 
 
-def _workspace(ws: Optional[torch.Tensor], need: int, dev: int, device) -> torch.Tensor:
+def _workspace(ws: Optional[torch.Tensor], need: int, dev: int, device) -> Optional[torch.Tensor]:
     if ws is None:
-        return torch.empty((need or 256,), dtype=torch.uint8, device=device)
+        return torch.empty((need,), dtype=torch.uint8, device=device) if need else None
     _check(ws, "workspace", dev, torch.uint8, (ws.numel(),))
     if ws.numel() < need:
         raise ValueError(f"workspace must hold {need} bytes, got {ws.numel()}")
@@ -493,13 +498,11 @@ def pack(fields: FieldList, x: torch.Tensor, stream=None) -> Packed:
     """An 8-bit checkpoint of x [n, C]."""
     t, dev = _table(fields), torch.cuda.current_device()
     n = _rows_of(x, "x", dev, t.C)
-    blocks = packed_blocks(t.fields) if t.blocks == 0 else t.blocks
     with _on(stream):
-        q = torch.empty((n, t.C), dtype=torch.int8, device=x.device)
-        exps = torch.empty((n, blocks), dtype=torch.uint8, device=x.device)
-    check(lib().ssconv_pack(t.ref, x.data_ptr(), _dtype(x), n, q.data_ptr(), exps.data_ptr(), _raw_stream(stream, dev)),
-          "ssconv_pack")
-    return Packed(t.fields, q, exps)
+        p = _new_packed(t, n, x)
+    check(lib().ssconv_pack(t.ref, x.data_ptr(), _dtype(x), n, p.q.data_ptr(), p.exps.data_ptr(),
+                            _raw_stream(stream, dev)), "ssconv_pack")
+    return p
 
 
 def unpack(p: Packed, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -509,7 +512,7 @@ def unpack(p: Packed, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, 
     _check_packed(p, "p", dev, t, n)
     if out is None:
         with _on(stream):
-            out = torch.empty((n, t.C), dtype=dtype, device=p.q.device)
+            out = p.q.new_empty((n, t.C), dtype=dtype)
     _check(out, "out", dev, dtype, (n, t.C))
     check(lib().ssconv_unpack(t.ref, p.q.data_ptr(), p.exps.data_ptr(), n, _dtype(out), out.data_ptr(),
                               _raw_stream(stream, dev)), "ssconv_unpack")
@@ -526,21 +529,21 @@ def site_norm_forward(fields: FieldList, x: Union[torch.Tensor, Packed], gain: O
     if isinstance(x, Packed):
         if checkpoint:
             raise ValueError("x is a checkpoint already")
-        n, device = x.q.shape[0], x.q.device
+        n = x.q.shape[0]
         dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
         r = _check_rows(x, "x", dev, t, n, None)
     else:
-        n, device = _rows_of(x, "x", dev, t.C), x.device
+        n = _rows_of(x, "x", dev, t.C)
         if dtype is not None and dtype != x.dtype:
             raise TypeError(f"the result of {x.dtype} rows is {x.dtype}, not {dtype}")
         dtype = x.dtype
         r = Rows(x.data_ptr(), None)
     with _on(stream):
         if out is None:
-            out = torch.empty((n, t.C), dtype=dtype, device=device)
+            out = x.q.new_empty((n, t.C), dtype=dtype) if isinstance(x, Packed) else torch.empty_like(x)
         else:
             _check(out, "out", dev, dtype, (n, t.C))
-        p = Packed.empty(t.fields, n, device) if checkpoint else None
+        p = _new_packed(t, n, x) if checkpoint else None
     check(lib().ssconv_site_norm_forward(t.ref, byref(r), _dtype(out), n, eps, g, out.data_ptr(),
                                          p.q.data_ptr() if p else None, p.exps.data_ptr() if p else None,
                                          _raw_stream(stream, dev)), "ssconv_site_norm_forward")
@@ -598,8 +601,8 @@ def residual_forward(fields: FieldList, y: torch.Tensor, h: torch.Tensor, scale:
         else:
             _check(out, "out", dev, dtype, shape)
         x_out = torch.empty_like(h) if next_norm else None
-        yp = Packed.empty(full.fields, n, h.device) if checkpoint else None
-        hp = Packed.empty(t.fields, n, h.device) if checkpoint and next_norm else None
+        yp = _new_packed(full, n, h) if checkpoint else None
+        hp = _new_packed(t, n, h) if checkpoint and next_norm else None
     check(lib().ssconv_residual_forward(t.ref, y.data_ptr(), h.data_ptr(), _dtype(h), n, eps, gp, s, gn, out.data_ptr(),
                                         x_out.data_ptr() if next_norm else None,
                                         yp.q.data_ptr() if yp else None, yp.exps.data_ptr() if yp else None,
@@ -632,7 +635,7 @@ def residual_backward(fields: FieldList, y: Union[torch.Tensor, Packed],
         raise ValueError("gain_next without dx")
     s, gp, gn = _param(scale, "scale", dev, t), _param(gain_post, "gain_post", dev, full), _param(gain_next, "gain_next", dev, t)
     with _on(stream):
-        dy = torch.empty((n, full.C), dtype=dtype, device=dh.device)
+        dy = dh.new_empty((n, full.C))
         dh_in = torch.empty_like(dh)
         ds = None if s is None else torch.empty_like(scale)
         dp = None if gp is None else torch.empty_like(gain_post)
@@ -688,7 +691,8 @@ def backward_packed(feats: Packed, grad_out: torch.Tensor, rb: Rulebook, W: torc
     check(lib().ssconv_backward_packed(t.ref, feats.q.data_ptr(), feats.exps.data_ptr(), int(bool(norm)), eps, g,
                                        grad_out.data_ptr(), _dtype(grad_out), cout, rb.handle, W.data_ptr(),
                                        byref(desc) if desc is not None else None, _ptr(basis), _ptr(gf), _ptr(gc),
-                                       ws.data_ptr(), ws.numel(), _raw_stream(stream, dev)), "ssconv_backward_packed")
+                                       _ptr(ws), 0 if ws is None else ws.numel(), _raw_stream(stream, dev)),
+          "ssconv_backward_packed")
     return gf, gc
 
 

@@ -115,15 +115,17 @@ int check_site(const ssconv_fields* fields, bool gated, ssconv_dtype dt, int64_t
 }
 
 int check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return SSCONV_OK;
   if (!ws || bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255))
     return fail(SSCONV_E_INVALID, "workspace must be 256-byte aligned and hold %zu bytes", need);
   return SSCONV_OK;
 }
 
-// A row of partial sums of every workgroup.
-size_t norm_ws_bytes(const SiteTab& t, int64_t n) { return (size_t)site_blocks(t, n, norm_bwd_per_cu) * t.C * 4; }
+// A row of partial sums of every workgroup; none where there is one.
+size_t part_bytes(unsigned blocks, int floats) { return blocks <= 1 ? 0 : (size_t)blocks * floats * 4; }
+size_t norm_ws_bytes(const SiteTab& t, int64_t n) { return part_bytes(bwd_blocks(t, n, norm_bwd_per_cu), t.C); }
 size_t tail_ws_bytes(const SiteTab& t, int64_t n) {
-  return (size_t)site_blocks(t, n, tail_bwd_per_cu) * (t.ch0[t.n] + 2 * t.C) * 4;
+  return part_bytes(bwd_blocks(t, n, tail_bwd_per_cu), t.ch0[t.n] + 2 * t.C);
 }
 
 }  // namespace
@@ -207,11 +209,14 @@ extern "C" int ssconv_site_norm_backward(const ssconv_fields* fields, const ssco
     a.eps = (float)eps;
     a.gain = gain;
     a.out = dx;
-    a.part = part;
+    const bool one = bwd_blocks(t, n, norm_bwd_per_cu) == 1;
+    a.part = one ? nullptr : part;
+    a.dgain = one ? dgain : nullptr;
     SSC_TRY(launch_norm_bwd(t, dtype, a, stream));
+    if (one) return SSCONV_OK;
   }
   const int F = dgain ? reduce_groups(t, t.n) : 0;
-  return reduce_fields(t, part, site_blocks(t, n, norm_bwd_per_cu), t.C, ReduceArgs{{dgain}, {0}, {F, F, F}}, stream);
+  return reduce_fields(t, part, bwd_blocks(t, n, norm_bwd_per_cu), t.C, ReduceArgs{{dgain}, {0}, {F, F, F}}, stream);
 }
 
 extern "C" int ssconv_residual_forward(const ssconv_fields* fields, const void* y, const void* h, ssconv_dtype dtype,
@@ -281,13 +286,18 @@ extern "C" int ssconv_residual_backward(const ssconv_fields* fields, const sscon
     a.gain_next = gain_next;
     a.dy = dy;
     a.dh_in = dh_in;
-    a.part = part;
+    const bool one = bwd_blocks(ty, n, tail_bwd_per_cu) == 1;
+    a.part = one ? nullptr : part;
+    a.grad[0] = one ? dgain_post : nullptr;
+    a.grad[1] = one ? dscale : nullptr;
+    a.grad[2] = one ? dgain_next : nullptr;
     SSC_TRY(launch_tail_bwd(ty, dtype, a, stream));
+    if (one) return SSCONV_OK;
   }
   const int F = reduce_groups(ty, ty.n_regular), FS = reduce_groups(ty, ty.n);
   ReduceArgs r{{dgain_post, dscale, dgain_next}, {0, S, S + C}, {}};
   r.end[0] = dgain_post ? FS : 0;
   r.end[1] = r.end[0] + (dscale ? F : 0);
   r.end[2] = r.end[1] + (dgain_next ? F : 0);
-  return reduce_fields(ty, part, site_blocks(ty, n, tail_bwd_per_cu), stride, r, stream);
+  return reduce_fields(ty, part, bwd_blocks(ty, n, tail_bwd_per_cu), stride, r, stream);
 }

@@ -62,6 +62,13 @@ inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int,
                                      256 * per_cu(site_lanes(t), site_chunks(t), t.ragged != 0));
 }
 
+// The backward's, whose workgroups each leave a row of partial sums of the parameters' gradients for a second launch.  Up
+// to two turns of one workgroup are left to one, which writes the gradients itself (backward of a tail of 8 rows of 104
+// channels, in passes that wait for the host: 22.4 us with the second launch and its workspace, 17.4 without).
+inline unsigned bwd_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
+  return n <= 2 * site_rows(t) ? (n > 0 ? 1u : 0u) : site_blocks(t, n, per_cu);
+}
+
 struct NormArgs {
   ssconv_rows x;
   const void *dy, *dres;
@@ -71,7 +78,8 @@ struct NormArgs {
   void* out;       // y, or dx
   int8_t* q;       // checkpoint of x (forward)
   uint8_t* exps;
-  float* part;     // [workgroups][C] (backward)
+  float* part;     // [workgroups][C] (backward); one workgroup writes dgain
+  float* dgain;
 };
 struct TailArgs {
   ssconv_rows y, h;  // h: h_out in the backward
@@ -83,7 +91,8 @@ struct TailArgs {
   int8_t *yq, *hq;
   uint8_t *ye, *he;
   void *dy, *dh_in;  // backward
-  float* part;       // [workgroups][S + 2 C]: post, scale, next
+  float* part;       // [workgroups][S + 2 C]: post, scale, next; one workgroup writes grad
+  float* grad[3];
 };
 
 int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st);

@@ -69,7 +69,8 @@ __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_
     for (int k = 0; k < K; ++k)
       if (on) w.template store<T>((T*)a.out + r0 * C, row, C, k, d[k] + res[k]);
   }
-  if (a.part) sum_rows<L, K, RAG>(w, acc, C, lds, a.part + (int64_t)blockIdx.x * C);
+  if (a.part || a.dgain)
+    sum_rows<L, K, RAG>(w, acc, C, lds, a.part ? a.part + (int64_t)blockIdx.x * C : nullptr, t, t.n, a.dgain);
 }
 
 template <typename T, int L, int K, bool RAG>
@@ -127,8 +128,8 @@ int launch_norm_fwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStr
 }
 
 int launch_norm_bwd(const SiteTab& t, ssconv_dtype dt, const NormArgs& a, hipStream_t st) {
-  const unsigned nb = site_blocks(t, a.n, norm_bwd_per_cu);
-  const size_t lds = a.part ? (size_t)site_rows(t) * t.ch0[t.n] * 4 : 0;
+  const unsigned nb = bwd_blocks(t, a.n, norm_bwd_per_cu);
+  const size_t lds = a.part || a.dgain ? (size_t)site_rows(t) * t.ch0[t.n] * 4 : 0;
   auto go = [&](auto kernel) {
     kernel<<<nb, kSiteNT, lds, st>>>(t, a);
     SSC_HIP(hipGetLastError());

@@ -602,11 +602,12 @@ __device__ __forceinline__ f8 lds_get(const Row<L, K, RAG>& w, int k, const floa
   return v;
 }
 
-// Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order, to out[channels];
-// lds holds one row of floats per row that the workgroup takes at a time.  All threads call it.
+// Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order; lds holds one row of
+// floats per row that the workgroup takes at a time.  All threads call it.  part: to part[channels]; else (the only
+// workgroup of its call) to grad, summed over the components of the fields of `entries` entries.
 template <int L, int K, bool RAG>
 __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc)[K], int channels, float* lds,
-                                         float* out) {
+                                         float* part, const SiteTab& t, int entries, float* grad) {
   constexpr int ROWS = kSiteNT / L;
   __syncthreads();
   float* mine = lds + ((threadIdx.x >> 6) * (64 / L) + w.sub) * channels;
@@ -620,7 +621,20 @@ __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc
     float s = 0.f;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) s += lds[r * channels + c];
-    out[c] = s;
+    if (part)
+      part[c] = s;
+    else
+      lds[c] = s;  // its column is this thread's
+  }
+  if (part || !grad) return;
+  __syncthreads();
+  for (int e = 0; e < entries; ++e) {
+    const int d = 2 * t.l[e] + 1;
+    for (int f = threadIdx.x; f < t.mult[e]; f += kSiteNT) {
+      float s = 0.f;
+      for (int i = 0; i < d; ++i) s += lds[t.ch0[e] + f * d + i];
+      grad[t.f0[e] + f] = s;
+    }
   }
 }
 

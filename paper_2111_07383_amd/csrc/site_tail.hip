@@ -186,15 +186,15 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
     for (int k = 0; k < K; ++k)
       if (on) w.template store<T>((T*)a.dy + r0 * S, row, S, k, e[k]);
   }
-  if (a.part) {
-    float* out = a.part + (int64_t)blockIdx.x * (S + 2 * C);
+  if (a.part || a.grad[0] || a.grad[1] || a.grad[2]) {
+    float* out = a.part ? a.part + (int64_t)blockIdx.x * (S + 2 * C) : nullptr;
     f8 s[K];
     w.params(a.scale, s, t.f0[t.n_regular]);
 #pragma unroll
     for (int k = 0; k < K; ++k) s[k] = main[k] ? s[k] * acc[k] : acc[k], acc[k] *= gp[k];
-    sum_rows<L, K, RAG>(w, s, S, lds, out);
-    sum_rows<L, K, RAG>(w, acc, C, lds, out + S);
-    sum_rows<L, K, RAG>(w, acc_n, C, lds, out + S + C);
+    sum_rows<L, K, RAG>(w, s, S, lds, out, t, t.n, a.grad[0]);
+    sum_rows<L, K, RAG>(w, acc, C, lds, out ? out + S : nullptr, t, t.n_regular, a.grad[1]);
+    sum_rows<L, K, RAG>(w, acc_n, C, lds, out ? out + S + C : nullptr, t, t.n_regular, a.grad[2]);
   }
 }
 
@@ -216,7 +216,7 @@ int launch_tail_fwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStr
 }
 
 int launch_tail_bwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStream_t st) {
-  const unsigned nb = site_blocks(t, a.n, tail_bwd_per_cu);
+  const unsigned nb = bwd_blocks(t, a.n, tail_bwd_per_cu);
   const int lds_row = site_lds_row(t);
   const size_t lds = (size_t)site_rows(t) * lds_row * 4;
   auto go = [&](auto kernel) {

@@ -496,7 +496,7 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         P.residual_backward(f, P.pack(f, x), x, x, x)    # a checkpoint of other fields
     with pytest.raises(ValueError):
-        P.site_norm_backward(f, x, x, ok, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+        P.site_norm_backward(f, x.repeat(99, 1), x.repeat(99, 1), ok, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         P.unpack(P.Packed(full, P.pack(f, x).q, P.pack(f, x).exps))
 
