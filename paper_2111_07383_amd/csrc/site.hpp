@@ -51,11 +51,11 @@ inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 // per SIMD.  All loop over the rows, so a grid of more would run in rounds of which the last is part empty (backward of
 // a 208-channel tail: 1024 workgroups of 144 registers, of which 768 fit, 235 us; the next version, 1024 of 128
 // registers, 127).  The norm's backward would hold 8; its partial sums then cost more (191.8k rows of 208 channels forward and
-// backward with 8 97 us, 6 94, 4 101).
+// backward with 8 97 us, 6 94, 4 101).  Backward of a tail of 60k rows of 312 channels: 3 85 us, 4 73.
 constexpr int norm_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 4 : K == 2 || rag ? 5 : 8; }
 constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
 constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }
-constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : K == 2 ? 2 : L == 64 ? 3 : 4; }
+constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : K == 2 ? 2 : L == 64 && rag ? 3 : 4; }
 inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
   const int64_t rows = site_rows(t);
   return (unsigned)std::min<int64_t>((n + rows - 1) / rows,

@@ -587,19 +587,18 @@ template <int L, int K, bool RAG>
 __device__ __forceinline__ void lds_put(const Row<L, K, RAG>& w, int k, float* buf, f8 v) {
   if constexpr (!RAG) {
     *reinterpret_cast<f8*>(buf + w.start[k]) = v;
+  } else if (w.hi[k] == 8) {
+    *reinterpret_cast<f8_any*>(buf + w.start[k]) = v;
   } else {
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
+    for (int c = 0; c < 7; ++c)
       if (c < w.hi[k]) buf[w.start[k] + c] = v[c];
   }
 }
 template <int L, int K, bool RAG>
 __device__ __forceinline__ f8 lds_get(const Row<L, K, RAG>& w, int k, const float* buf) {  // the buffer ends 8 past the row
   if constexpr (!RAG) return *reinterpret_cast<const f8*>(buf + w.start[k]);
-  f8 v;
-#pragma unroll
-  for (int c = 0; c < 8; ++c) v[c] = buf[w.start[k] + c];
-  return v;
+  return *reinterpret_cast<const f8_any*>(buf + w.start[k]);
 }
 
 // Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order; lds holds one row of
