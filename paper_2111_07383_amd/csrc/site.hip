@@ -36,7 +36,7 @@ int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t) {
     fi += t->mult[e];
     b += (w + kPackBlock - 1) / kPackBlock;
     tc += (w + kChunk - 1) / kChunk;
-    if (w % kChunk) t->ragged = 1;
+    if (w % kChunk) t->ragged = std::max(t->ragged, w < kChunk ? 2 : 1);
   }
   for (int e = t->n; e <= SSCONV_MAX_ENTRIES; ++e)
     t->ch0[e] = (int)ch, t->f0[e] = (int)fi, t->b0[e] = (int)b, t->t0[e] = (int)tc;

@@ -27,7 +27,7 @@ struct SiteTab {
   float m[SSCONV_MAX_ENTRIES], rm[SSCONV_MAX_ENTRIES];  // fields, and 1 / fields
   int C, G;                         // channels without the gates, gates
   int n_regular;                    // entries without the gates'
-  int ragged;                       // some entry is not a multiple of 8 channels
+  int ragged;                       // 1: some entry is no multiple of 8 channels, 2: some entry has fewer
 };
 
 // gated: the gates of the fields of order > 0 as one more entry.
@@ -52,20 +52,20 @@ inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 // a 208-channel tail: 1024 workgroups of 144 registers, of which 768 fit, 235 us; the next version, 1024 of 128
 // registers, 127).  The norm's backward would hold 8; its partial sums then cost more (191.8k rows of 208 channels forward and
 // backward with 8 97 us, 6 94, 4 101).  Backward of a tail of 60k rows of 312 channels: 3 85 us, 4 73.
-constexpr int norm_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 4 : K == 2 || rag ? 5 : 8; }
-constexpr int norm_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
-constexpr int tail_fwd_per_cu(int L, int K, bool rag) { return K == 3 ? 2 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }
-constexpr int tail_bwd_per_cu(int L, int K, bool rag) { return K == 3 ? 1 : K == 2 ? 2 : L == 64 && rag ? 3 : 4; }
-inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
+constexpr int norm_fwd_per_cu(int L, int K, int rag) { return K == 3 ? 4 : K == 2 || rag ? 5 : 8; }
+constexpr int norm_bwd_per_cu(int L, int K, int rag) { return K == 3 ? 2 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
+constexpr int tail_fwd_per_cu(int L, int K, int rag) { return K == 3 ? 2 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }
+constexpr int tail_bwd_per_cu(int L, int K, int rag) { return K == 3 ? 1 : K == 2 ? 2 : L == 64 && rag ? 3 : 4; }
+inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, int)) {
   const int64_t rows = site_rows(t);
   return (unsigned)std::min<int64_t>((n + rows - 1) / rows,
-                                     256 * per_cu(site_lanes(t), site_chunks(t), t.ragged != 0));
+                                     256 * per_cu(site_lanes(t), site_chunks(t), t.ragged));
 }
 
 // The backward's, whose workgroups each leave a row of partial sums of the parameters' gradients for a second launch.  Up
 // to two turns of one workgroup are left to one, which writes the gradients itself (backward of a tail of 8 rows of 104
 // channels, in passes that wait for the host: 22.4 us with the second launch and its workspace, 17.4 without).
-inline unsigned bwd_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, bool)) {
+inline unsigned bwd_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, int)) {
   return n <= 2 * site_rows(t) ? (n > 0 ? 1u : 0u) : site_blocks(t, n, per_cu);
 }
 

@@ -6,7 +6,7 @@
 namespace ssconv {
 namespace {
 
-template <typename T, int L, int K, bool RAG, bool PK>
+template <typename T, int L, int K, int RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void norm_fwd_kernel(SiteTab t, NormArgs a) {
   using R = Row<L, K, RAG>;
   R w;
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void norm_fwd_
   }
 }
 
-template <typename T, int L, int K, bool RAG, bool PK>
+template <typename T, int L, int K, int RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_kernel(SiteTab t, NormArgs a) {
   extern __shared__ float lds[];
   using R = Row<L, K, RAG>;
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_
     sum_rows<L, K, RAG>(w, acc, C, lds, a.part ? a.part + (int64_t)blockIdx.x * C : nullptr, t, t.n, a.dgain);
 }
 
-template <typename T, int L, int K, bool RAG>
+template <typename T, int L, int K, int RAG>
 __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kernel(SiteTab t, const T* x, int64_t n, int8_t* q, uint8_t* exps) {
   using R = Row<L, K, RAG>;
   R w;
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kern
   }
 }
 
-template <typename T, int L, int K, bool RAG>
+template <typename T, int L, int K, int RAG>
 __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void unpack_kernel(SiteTab t, const int8_t* q, const uint8_t* exps, int64_t n,
                                                          T* x) {
   using R = Row<L, K, RAG>;

@@ -2,10 +2,11 @@
 //
 // A row is L lanes' of a wavefront (64 / L rows each), every lane holding K chunks of 8 channels of one entry each.
 // Loads and stores are one 16-byte access a chunk (bf16; two in fp32, 8 bytes of a checkpoint) at whatever alignment
-// the row has, so nothing passes through LDS but what lanes owe each other.  An entry that is no multiple of 8 ends in
-// a chunk moved back to its end: its first `lo` channels are the previous chunk's too, take part in no sum and are
-// computed and stored twice, with the same bits.  Entries under 8 channels have one chunk of `hi` channels, moved
-// element by element.
+// the row has, so nothing passes through LDS but what lanes owe each other.  RAG = 1: an entry that is no multiple of 8
+// ends in a chunk moved back to its end: its first `lo` channels are the previous chunk's too, take part in no sum and are
+// computed and stored twice, with the same bits.  RAG = 2: entries under 8 channels have one chunk of `hi` channels, moved
+// element by element, which every chunk then has branches for (backward of a tail of 60k rows of 303 channels without
+// narrow entries: 126 us with them, 94 without).
 //
 // With K = 1 an entry is a run of lanes, and its sums are a segmented prefix sum (3 to 6 DPP additions, whatever the
 // number of entries) of which the run's last lane is read back; with K = 2 or 3 (rows over 64 or 128 chunks) they are sums
@@ -101,7 +102,7 @@ __device__ __forceinline__ int64_t first_row() {
   return ((int64_t)blockIdx.x * (kSiteNT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * ROWS;
 }
 
-template <int L, int K, bool RAG>
+template <int L, int K, int RAG>
 struct Row {
   static constexpr int R = 64 / L;            // rows of a wavefront
   static constexpr int Q = K == 1 ? 2 : 4;    // gates of a lane: a row of 8 L K channels has at most 2 L K of them
@@ -146,9 +147,9 @@ struct Row {
         int s = at, first = 0, end = 8;
         if (RAG) {
           const bool over = at + 8 > w;
-          s = over ? max(w - 8, 0) : at;
+          s = over ? (RAG == 2 ? max(w - 8, 0) : w - 8) : at;
           first = at - s;
-          end = min(w, 8);
+          if (RAG == 2) end = min(w, 8);
         }
         start[k] = in ? ch0 + s : start[k];
         rel[k] = in ? s : rel[k];
@@ -189,13 +190,13 @@ struct Row {
   __device__ __forceinline__ int row_of(int64_t left) const { return min(sub, (int)min(left, (int64_t)R) - 1); }
 
   // The channels of a chunk, of row r of a matrix of C channels, from channel s on (start[k], or 0 where the chunk lies
-  // past a matrix without the gates).  Without ragged entries a lane with no chunk there reads the row's first channels,
+  // past a matrix without the gates).  Without narrow entries a lane with no chunk there reads the row's first channels,
   // which nothing uses; else it has zeros.
   template <typename T>
   __device__ __forceinline__ f8 load(const void* p, int r, int C, int k, int s) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
     const T* q = reinterpret_cast<const T*>((const char*)p + (__umul24(r, C) + s) * (uint32_t)sizeof(T));
-    if (!RAG || hi[k] == 8) {
+    if (RAG < 2 || hi[k] == 8) {
       v = load8<T>(q);
     } else {
 #pragma unroll
@@ -211,10 +212,10 @@ struct Row {
                                             float& scale) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
     scale = 1.f;
-    if (RAG && hi[k] == 0) return v;
+    if (RAG == 2 && hi[k] == 0) return v;
     const int8_t* at = (const int8_t*)p + (uint32_t)(__umul24(r, C) + s);
     u2 q = {0, 0};
-    if (!RAG || hi[k] == 8) {
+    if (RAG < 2 || hi[k] == 8) {
       q = *reinterpret_cast<const u2_any*>(at);
     } else {
 #pragma unroll
@@ -228,10 +229,11 @@ struct Row {
       scale = x;
       return v;
     }
-    const float x_lo = lo[k] > 0 ? pack_scale(b[(uint32_t)(__umul24(r, B) + blk_lo[k])]) : x;
+    const int to_lo = s == start[k] ? blk_lo[k] : bl;  // a lane that reads elsewhere uses nothing of it
+    const float x_lo = pack_scale(b[(uint32_t)(__umul24(r, B) + to_lo)]);
 #pragma unroll
     for (int c = 0; c < 8; ++c) v[c] *= c < lo[k] ? x_lo : x;
-    if (hi[k] < 8)  // 0 * NaN
+    if (RAG == 2 && hi[k] < 8)  // 0 * NaN
 #pragma unroll
       for (int c = 1; c < 8; ++c)
         if (c >= hi[k]) v[c] = 0.f;
@@ -251,7 +253,7 @@ struct Row {
   template <typename T>
   __device__ __forceinline__ void store(void* p, int r, int C, int k, f8 v) const {
     T* q = reinterpret_cast<T*>((char*)p + (__umul24(r, C) + start[k]) * (uint32_t)sizeof(T));
-    if (!RAG || hi[k] == 8) {
+    if (RAG < 2 || hi[k] == 8) {
       if (hi[k]) store8(q, v);
     } else {
 #pragma unroll
@@ -260,7 +262,7 @@ struct Row {
     }
   }
 
-  __device__ __forceinline__ bool counts(int k, int c) const { return !RAG || (c >= lo[k] && c < hi[k]); }
+  __device__ __forceinline__ bool counts(int k, int c) const { return !RAG || (c >= lo[k] && (RAG == 1 || c < hi[k])); }
 
   __device__ __forceinline__ float of(f8 v, int k) const {  // sum of the chunk's channels that count
     float s[8];
@@ -505,7 +507,7 @@ struct Row {
 };
 
 // The gates of a row, shared out over its lanes: gate i + q L of the row has components [c0, c0 + d) of the fields.
-template <int L, int K, bool RAG>
+template <int L, int K, int RAG>
 struct Gates {
   static constexpr int Q = Row<L, K, RAG>::Q;
   int c0[Q], d[Q], at[Q];  // d = 0: none; at: the gate's own channel
@@ -583,11 +585,11 @@ struct Gates {
 };
 
 // 8 channels of a row in LDS; those past hi (where the chunk is no whole one) are left alone.
-template <int L, int K, bool RAG>
+template <int L, int K, int RAG>
 __device__ __forceinline__ void lds_put(const Row<L, K, RAG>& w, int k, float* buf, f8 v) {
   if constexpr (!RAG) {
     *reinterpret_cast<f8*>(buf + w.start[k]) = v;
-  } else if (w.hi[k] == 8) {
+  } else if (RAG == 1 || w.hi[k] == 8) {
     *reinterpret_cast<f8_any*>(buf + w.start[k]) = v;
   } else {
 #pragma unroll
@@ -595,7 +597,7 @@ __device__ __forceinline__ void lds_put(const Row<L, K, RAG>& w, int k, float* b
       if (c < w.hi[k]) buf[w.start[k] + c] = v[c];
   }
 }
-template <int L, int K, bool RAG>
+template <int L, int K, int RAG>
 __device__ __forceinline__ f8 lds_get(const Row<L, K, RAG>& w, int k, const float* buf) {  // the buffer ends 8 past the row
   if constexpr (!RAG) return *reinterpret_cast<const f8*>(buf + w.start[k]);
   return *reinterpret_cast<const f8_any*>(buf + w.start[k]);
@@ -604,7 +606,7 @@ __device__ __forceinline__ f8 lds_get(const Row<L, K, RAG>& w, int k, const floa
 // Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order; lds holds one row of
 // floats per row that the workgroup takes at a time.  All threads call it.  part: to part[channels]; else (the only
 // workgroup of its call) to grad, summed over the components of the fields of `entries` entries.
-template <int L, int K, bool RAG>
+template <int L, int K, int RAG>
 __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc)[K], int channels, float* lds,
                                          float* part, const SiteTab& t, int entries, float* grad) {
   constexpr int ROWS = kSiteNT / L;
@@ -638,23 +640,21 @@ __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc
 }
 
 // GO_(L, K, RAG) for a table.
-#define SSK_SITE_DISPATCH(t_, GO_)                                   \
-  do {                                                               \
-    const int chunks_ = (t_).t0[(t_).n];                             \
-    if ((t_).ragged) {                                               \
-      if (chunks_ <= 8) GO_(8, 1, true);                             \
-      if (chunks_ <= 16) GO_(16, 1, true);                           \
-      if (chunks_ <= 32) GO_(32, 1, true);                           \
-      if (chunks_ <= 64) GO_(64, 1, true);                           \
-      if (chunks_ <= 128) GO_(64, 2, true);                          \
-      GO_(64, 3, true);                                              \
-    }                                                                \
-    if (chunks_ <= 8) GO_(8, 1, false);                              \
-    if (chunks_ <= 16) GO_(16, 1, false);                            \
-    if (chunks_ <= 32) GO_(32, 1, false);                            \
-    if (chunks_ <= 64) GO_(64, 1, false);                            \
-    if (chunks_ <= 128) GO_(64, 2, false);                           \
-    GO_(64, 3, false);                                               \
+#define SSK_SITE_DISPATCH(t_, GO_)               \
+  do {                                           \
+    const int chunks_ = (t_).t0[(t_).n];         \
+    if ((t_).ragged == 2) SSK_SITE_MODE(GO_, 2); \
+    if ((t_).ragged == 1) SSK_SITE_MODE(GO_, 1); \
+    SSK_SITE_MODE(GO_, 0);                       \
+  } while (0)
+#define SSK_SITE_MODE(GO_, R_)                \
+  do {                                        \
+    if (chunks_ <= 8) GO_(8, 1, R_);          \
+    if (chunks_ <= 16) GO_(16, 1, R_);        \
+    if (chunks_ <= 32) GO_(32, 1, R_);        \
+    if (chunks_ <= 64) GO_(64, 1, R_);        \
+    if (chunks_ <= 128) GO_(64, 2, R_);       \
+    GO_(64, 3, R_);                           \
   } while (0)
 
 }  // namespace ssconv

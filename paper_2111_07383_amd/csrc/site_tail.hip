@@ -10,7 +10,7 @@ namespace {
 
 constexpr f8 kZero = {0, 0, 0, 0, 0, 0, 0, 0}, kOne = {1, 1, 1, 1, 1, 1, 1, 1};
 
-template <typename T, int L, int K, bool RAG>
+template <typename T, int L, int K, int RAG>
 __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_kernel(SiteTab t, TailArgs a, int lds_row) {
   extern __shared__ __attribute__((aligned(32))) float lds[];
   using R = Row<L, K, RAG>;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
     for (int k = 0; k < K; ++k) {
       y[k] = w.template load<T>((const T*)a.y.data + r0 * S, row, S, k, w.start[k]);
       h[k] = kZero;
-      if (!RAG || main[k]) h[k] = w.template load<T>((const T*)a.h.data + r0 * C, row, C, k, at[k]);
+      if (RAG < 2 || main[k]) h[k] = w.template load<T>((const T*)a.h.data + r0 * C, row, C, k, at[k]);
     }
     if (a.yq) w.pack(y, a.yq + r0 * S, a.ye + r0 * By, row, S, By, t.n, on);
     w.norm(y, r, a.eps);
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
 // parameters of the block's output are the same sum over the rows: dscale = gain_post sum(e yhat),
 // dgain_post = scale sum(e yhat); and what goes on behind the norm is scale gain_post e.  The components of a field
 // share both parameters, so its gate's lane multiplies their sum of dh u by the scale.
-template <typename T, int L, int K, bool RAG, bool PK>
+template <typename T, int L, int K, int RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_kernel(SiteTab t, TailArgs a, int lds_row) {
   extern __shared__ __attribute__((aligned(32))) float lds[];
   using R = Row<L, K, RAG>;
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
       y[k] = w.template load_rows<T, PK>(a.y, r0, row, S, By, k, w.start[k], w.blk[k], ys[k]);
       e[k] = h[k] = dx[k] = kZero;
       hs[k] = 1.f;
-      if (RAG && !main[k]) continue;
+      if (RAG == 2 && !main[k]) continue;
       e[k] = w.template load<T>((const T*)a.dh + r0 * C, row, C, k, at[k]);
       if (!a.dx) continue;
       dx[k] = w.template load<T>((const T*)a.dx + r0 * C, row, C, k, at[k]);

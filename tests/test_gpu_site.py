@@ -42,6 +42,12 @@ FIELDS = {
     "w510": ((1, 127),),                             # 381 + 127
     "w900": ((0, 500), (1, 100), (2, 10)),           # 850 + 110
     "w1024": ((0, 496), (1, 100), (2, 16), (0, 32)),  # 908 + 116: all of the 1024, 129 chunks of 8
+    # an entry under 8 channels in rows of more lanes and more chunks a lane
+    "narrow16": ((0, 60), (1, 5), (2, 1)),
+    "narrow32": ((0, 130), (1, 5), (2, 1), (0, 3)),
+    "narrow64": ((0, 3), (0, 300), (1, 20), (2, 1)),
+    "narrow128": ((0, 600), (1, 7), (2, 1), (0, 150)),
+    "narrow192": ((0, 3), (0, 770), (1, 60), (2, 1)),  # 958 + 61: 130 chunks of 8
 }
 NORM_ONLY = {"eight": ((0, 3), (1, 2)) * 4, "all1024": ((0, 1024),), "vec1023": ((1, 341),),
              "odd1023": ((0, 129),) * 7 + ((0, 120),)}
