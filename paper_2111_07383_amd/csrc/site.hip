@@ -21,25 +21,34 @@ int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t) {
     t->mult[t->n] = t->G;
     ++t->n;
   }
-  int64_t ch = 0, fi = 0, b = 0, tc = 0;
+  int64_t ch = 0, fi = 0, b = 0;
   for (int e = 0; e < t->n; ++e) {
     const int64_t w = (int64_t)t->mult[e] * (2 * t->l[e] + 1);
     if (ch + w > kSiteMaxC) return fail(SSCONV_E_INVALID, "a row has at most %d channels", kSiteMaxC);
     t->ch0[e] = (int)ch;
     t->f0[e] = (int)fi;
     t->b0[e] = (int)b;
-    t->t0[e] = (int)tc;
     t->inv[e] = 65536 / (2 * t->l[e] + 1) + 1;
     t->m[e] = (float)t->mult[e];
     t->rm[e] = 1.f / t->m[e];
     ch += w;
     fi += t->mult[e];
     b += (w + kPackBlock - 1) / kPackBlock;
-    tc += (w + kChunk - 1) / kChunk;
-    if (w % kChunk) t->ragged = std::max(t->ragged, w < kChunk ? 2 : 1);
   }
   for (int e = t->n; e <= SSCONV_MAX_ENTRIES; ++e)
-    t->ch0[e] = (int)ch, t->f0[e] = (int)fi, t->b0[e] = (int)b, t->t0[e] = (int)tc;
+    t->ch0[e] = (int)ch, t->f0[e] = (int)fi, t->b0[e] = (int)b;
+  for (t->K = 1;; t->K *= 2) {  // K = 4 fits: at most 1024 / 32 lanes and one more an entry
+    int lanes = 0;
+    t->ragged = 0;
+    for (int e = 0; e < t->n; ++e) {
+      const int w = t->ch0[e + 1] - t->ch0[e], per = kChunk * t->K;
+      t->t0[e] = lanes;
+      lanes += (w + per - 1) / per;
+      if (w % per) t->ragged = std::max(t->ragged, w < kChunk ? 2 : 1);
+    }
+    for (int e = t->n; e <= SSCONV_MAX_ENTRIES; ++e) t->t0[e] = lanes;
+    if (lanes <= 64) break;
+  }
   return SSCONV_OK;
 }
 

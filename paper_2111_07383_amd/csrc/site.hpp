@@ -13,7 +13,9 @@ constexpr int kChunk = 8;       // channels that a lane holds at a time
 constexpr int kSiteNT = 256;
 
 // Entries of a row (those of a field list, and behind them the gates of a residual block as one more).  Every entry is
-// cut into chunks of 8 channels of its own.
+// cut into chunks of 8 channels of its own, K of which a lane holds: 1, 2 or 4, the least that fits 64 lanes.  (Two chunks
+// on half the lanes share out the sums over more channels, but take twice the registers and leave gaps between the
+// lanes' loads: backward of a tail of 100k rows of 104 channels 39 us with one, 77 with two; of 208 channels 68 and 80.)
 struct SiteTab {
   int n;                            // entries
   int l[SSCONV_MAX_ENTRIES];
@@ -21,13 +23,14 @@ struct SiteTab {
   int ch0[SSCONV_MAX_ENTRIES + 1];  // first channel of each entry, ch0[n] = channels
   int f0[SSCONV_MAX_ENTRIES + 1];   // first field
   int b0[SSCONV_MAX_ENTRIES + 1];   // first checkpoint block, b0[n] = blocks of a row
-  int t0[SSCONV_MAX_ENTRIES + 1];   // first chunk, t0[n] = chunks of a row
+  int K;                            // chunks of a lane
+  int t0[SSCONV_MAX_ENTRIES + 1];   // first lane, t0[n] = lanes that a row needs
   int gate0[SSCONV_MAX_ENTRIES];    // gate of the first field of each entry (entries of order > 0)
   int inv[SSCONV_MAX_ENTRIES];      // 65536 / components + 1: channel -> field without a division
   float m[SSCONV_MAX_ENTRIES], rm[SSCONV_MAX_ENTRIES];  // fields, and 1 / fields
   int C, G;                         // channels without the gates, gates
   int n_regular;                    // entries without the gates'
-  int ragged;                       // 1: some entry is no multiple of 8 channels, 2: some entry has fewer
+  int ragged;                       // 1: some entry is no multiple of 8 K channels, 2: some entry has fewer than 8
 };
 
 // gated: the gates of the fields of order > 0 as one more entry.
@@ -41,7 +44,6 @@ inline int site_lanes(const SiteTab& t) {
   const int c = t.t0[t.n];
   return c <= 8 ? 8 : c <= 16 ? 16 : c <= 32 ? 32 : 64;
 }
-inline int site_chunks(const SiteTab& t) { return t.t0[t.n] <= 64 ? 1 : t.t0[t.n] <= 128 ? 2 : 3; }
 // Floats of LDS per row of the residual tail: the row, and 8 that a chunk moved off it may read.
 inline int site_lds_row(const SiteTab& t) { return (t.ch0[t.n] + 8 + 7) / 8 * 8; }
 // Rows that a workgroup takes at a time.
@@ -52,14 +54,14 @@ inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 // a 208-channel tail: 1024 workgroups of 144 registers, of which 768 fit, 235 us; the next version, 1024 of 128
 // registers, 127).  The norm's backward would hold 8; its partial sums then cost more (191.8k rows of 208 channels forward and
 // backward with 8 97 us, 6 94, 4 101).  Backward of a tail of 60k rows of 312 channels: 3 85 us, 4 73.
-constexpr int norm_fwd_per_cu(int L, int K, int rag) { return K == 3 ? 4 : K == 2 || rag ? 5 : 8; }
-constexpr int norm_bwd_per_cu(int L, int K, int rag) { return K == 3 ? 2 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
-constexpr int tail_fwd_per_cu(int L, int K, int rag) { return K == 3 ? 2 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }
-constexpr int tail_bwd_per_cu(int L, int K, int rag) { return K == 3 ? 1 : K == 2 ? 2 : L == 64 && rag ? 3 : 4; }
+constexpr int norm_fwd_per_cu(int L, int K, int rag) { return K == 4 ? 2 : K == 2 || rag ? 5 : 8; }
+constexpr int norm_bwd_per_cu(int L, int K, int rag) { return K == 4 ? 1 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
+constexpr int tail_fwd_per_cu(int L, int K, int rag) { return K == 4 ? 1 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }
+constexpr int tail_bwd_per_cu(int L, int K, int rag) { return K == 4 ? 1 : K == 2 ? 2 : L == 64 && rag ? 3 : 4; }
 inline unsigned site_blocks(const SiteTab& t, int64_t n, int (*per_cu)(int, int, int)) {
   const int64_t rows = site_rows(t);
   return (unsigned)std::min<int64_t>((n + rows - 1) / rows,
-                                     256 * per_cu(site_lanes(t), site_chunks(t), t.ragged));
+                                     256 * per_cu(site_lanes(t), t.K, t.ragged));
 }
 
 // The backward's, whose workgroups each leave a row of partial sums of the parameters' gradients for a second launch.  Up

@@ -19,7 +19,7 @@ __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void norm_fwd_
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
     f8 x[K];
-    float r[K], xs[K];
+    float r, xs[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = w.template load_rows<T, PK>(a.x, r0, row, C, B, k, w.start[k], w.blk[k], xs[k]);
     if (a.q) w.pack(x, a.q + r0 * C, a.exps + r0 * B, row, C, B, t.n, on);
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
     f8 x[K], d[K], res[K];
-    float r[K], xs[K];
+    float r, xs[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       x[k] = w.template load_rows<T, PK>(a.x, r0, row, C, B, k, w.start[k], w.blk[k], xs[k]);

@@ -8,9 +8,10 @@
 // element by element, which every chunk then has branches for (backward of a tail of 60k rows of 303 channels without
 // narrow entries: 126 us with them, 94 without).
 //
-// With K = 1 an entry is a run of lanes, and its sums are a segmented prefix sum (3 to 6 DPP additions, whatever the
-// number of entries) of which the run's last lane is read back; with K = 2 or 3 (rows over 64 or 128 chunks) they are sums
-// over the wavefront entry by entry.
+// An entry begins with a lane, so it is a run of lanes; what its last lane has no chunk for is left empty.  Its sums are
+// a segmented prefix sum (3 to 6 DPP additions, whatever the number of entries) of which the run's last lane is read
+// back.  (With two chunks a lane, summing over the wavefront entry by entry made the tail of 60k rows of 480 channels
+// 87 us forward and 211 backward; this way 69 and 149.)
 #pragma once
 
 #include "site.hpp"
@@ -48,17 +49,6 @@ __device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_r
 template <int CTRL>
 __device__ __forceinline__ float dpp_or_0(float v) {  // the value of another lane, 0 where there is none
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-
-// Sum over the wavefront, in a scalar register.
-__device__ __forceinline__ float wave_total(float v) {
-  v += dpp_or_0<0x111>(v);  // the lane 1, 2, 4, 8 before
-  v += dpp_or_0<0x112>(v);
-  v += dpp_or_0<0x114>(v);
-  v += dpp_or_0<0x118>(v);
-  v += dpp_or_0<0x142>(v);  // lane 15 of the 16 before
-  v += dpp_or_0<0x143>(v);  // lane 31
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 __device__ __forceinline__ float read_lane(float v, int addr) {
@@ -105,84 +95,82 @@ __device__ __forceinline__ int64_t first_row() {
 template <int L, int K, int RAG>
 struct Row {
   static constexpr int R = 64 / L;            // rows of a wavefront
-  static constexpr int Q = K == 1 ? 2 : 4;    // gates of a lane: a row of 8 L K channels has at most 2 L K of them
+  static constexpr int Q = 2 * K;             // gates of a lane: a row of 8 L K channels has at most 2 L K of them
+  static constexpr int M = 4 / K;             // lanes of a checkpoint's block
   int i, sub;                       // lane of the row, row of the wavefront
   int start[K];                     // first channel of the chunk
   int lo[K], hi[K];                 // its channels that count: [lo, hi); those under hi exist; hi = 0: no chunk
-  int e[K];                         // entry
-  int rel[K], f0[K], inv[K];        // first channel within the entry, first field of the entry, 65536 / components + 1
-  int blk[K], blk_lo[K], quad[K];   // exponent byte, that of the channels under lo, place of the chunk in its block
-  float m[K], rm[K];                // fields of the entry, and 1 / m
-  bool scalar[K];
+  int rel[K];                       // first channel within the entry
+  int blk[K], blk_lo[K];            // exponent byte, that of the channels under lo
+  int e, f0, inv;                   // entry, its first field, 65536 / components + 1
+  float m, rm;                      // fields of the entry, and 1 / m
+  bool scalar;
   bool any_scalar;                  // uniform
-  int n;
-  int last;                         // ds_bpermute address of the last lane of the run (K = 1)
-  int mate[3];                      // and of the lanes of the same block
+  bool first;                       // of the lanes of its block
+  int last;                         // ds_bpermute address of the last lane of the run
+  int mate[3];                      // and of the other lanes of the block
   float m1, m2, m4, m8, m15, m31;   // 1 where the lane that many places before belongs to the run
 
   __device__ __forceinline__ void init(const SiteTab& t, int entries) {
     const int lane = threadIdx.x & 63;
     i = lane & (L - 1);
     sub = lane / L;
-    n = entries;
-    any_scalar = false;
-    int seg0 = i, seg1 = i;  // a lane without a chunk is a run of its own
+    any_scalar = scalar = false;
+    int seg0 = i, seg1 = i;  // a lane without an entry is a run of its own
+    e = -1;
+    f0 = 0;
+    inv = 65537;
+    m = rm = 1.f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      start[k] = lo[k] = hi[k] = rel[k] = f0[k] = blk[k] = blk_lo[k] = quad[k] = 0;
-      e[k] = -1;
-      inv[k] = 65537;
-      m[k] = rm[k] = 1.f;
-      scalar[k] = false;
-    }
+    for (int k = 0; k < K; ++k) start[k] = hi[k] = rel[k] = blk[k] = blk_lo[k] = 0, lo[k] = 8;
 #pragma unroll
     for (int en = 0; en < SSCONV_MAX_ENTRIES; ++en) {
       if (en >= entries) break;
       const int t0 = t.t0[en], t1 = t.t0[en + 1], ch0 = t.ch0[en], w = t.ch0[en + 1] - ch0;
       any_scalar |= t.l[en] == 0;
+      const bool in = i >= t0 && i < t1;
+      e = in ? en : e;
+      inv = in ? t.inv[en] : inv;
+      f0 = in ? t.f0[en] : f0;
+      m = in ? t.m[en] : m;
+      rm = in ? t.rm[en] : rm;
+      scalar = in ? t.l[en] == 0 : scalar;
+      seg0 = in ? t0 : seg0;
+      seg1 = in ? t1 - 1 : seg1;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int c = i + k * L, j = c - t0, at = 8 * j;
-        const bool in = c >= t0 && c < t1;
-        int s = at, first = 0, end = 8;
+        const int j = (i - t0) * K + k, at = 8 * j;
+        const bool here = RAG ? in && at < w : in;
+        int s = at, skip = 0, end = 8;
         if (RAG) {
           const bool over = at + 8 > w;
           s = over ? (RAG == 2 ? max(w - 8, 0) : w - 8) : at;
-          first = at - s;
+          skip = at - s;
           if (RAG == 2) end = min(w, 8);
         }
-        start[k] = in ? ch0 + s : start[k];
-        rel[k] = in ? s : rel[k];
-        lo[k] = in ? first : lo[k];
-        hi[k] = in ? end : hi[k];
-        e[k] = in ? en : e[k];
-        inv[k] = in ? t.inv[en] : inv[k];
-        f0[k] = in ? t.f0[en] : f0[k];
-        blk[k] = in ? t.b0[en] + j / 4 : blk[k];
-        blk_lo[k] = in ? t.b0[en] + max(j - 1, 0) / 4 : blk_lo[k];
-        quad[k] = in ? j & 3 : quad[k];
-        m[k] = in ? t.m[en] : m[k];
-        rm[k] = in ? t.rm[en] : rm[k];
-        scalar[k] = in ? t.l[en] == 0 : scalar[k];
-        if (k == 0) seg0 = in ? t0 : seg0, seg1 = in ? t1 - 1 : seg1;
+        start[k] = here ? ch0 + s : start[k];
+        rel[k] = here ? s : rel[k];
+        lo[k] = here ? skip : lo[k];
+        hi[k] = here ? end : hi[k];
+        blk[k] = here ? t.b0[en] + j / 4 : blk[k];
+        blk_lo[k] = here ? t.b0[en] + max(j - 1, 0) / 4 : blk_lo[k];
       }
     }
-    if (K == 1) {
-      const int base = lane - i;
-      last = 4 * (base + seg1);
-      m1 = i - 1 >= seg0 ? 1.f : 0.f;
-      m2 = i - 2 >= seg0 ? 1.f : 0.f;
-      m4 = i - 4 >= seg0 ? 1.f : 0.f;
-      m8 = i - 8 >= seg0 ? 1.f : 0.f;
-      m15 = (i & 16) && seg0 < (i & ~15) ? 1.f : 0.f;
-      m31 = i >= 32 && seg0 < 32 ? 1.f : 0.f;
+    const int base = lane - i, in_block = (i - seg0) & (M - 1);
+    first = in_block == 0;
+    last = 4 * (base + seg1);
+    m1 = i - 1 >= seg0 ? 1.f : 0.f;
+    m2 = i - 2 >= seg0 ? 1.f : 0.f;
+    m4 = i - 4 >= seg0 ? 1.f : 0.f;
+    m8 = i - 8 >= seg0 ? 1.f : 0.f;
+    m15 = (i & 16) && seg0 < (i & ~15) ? 1.f : 0.f;
+    m31 = i >= 32 && seg0 < 32 ? 1.f : 0.f;
 #pragma unroll
-      for (int b = 0; b < 3; ++b) mate[b] = 4 * (base + min(i - quad[0] + ((quad[0] + b + 1) & 3), seg1));
-    }
+    for (int b = 0; b < 3; ++b) mate[b] = 4 * (base + min(i - in_block + ((in_block + b + 1) & (M - 1)), seg1));
   }
 
   __device__ __forceinline__ int field(int k, int v) const {  // of channel v of the chunk, in its entry; < 1024 channels
-    return ((rel[k] + v) * inv[k]) >> 16;
+    return ((rel[k] + v) * inv) >> 16;
   }
 
   // Every matrix is addressed from the wavefront's first row (scalar registers) by 32-bit offsets of the lanes.  Rows
@@ -264,143 +252,132 @@ struct Row {
 
   __device__ __forceinline__ bool counts(int k, int c) const { return !RAG || (c >= lo[k] && (RAG == 1 || c < hi[k])); }
 
-  __device__ __forceinline__ float of(f8 v, int k) const {  // sum of the chunk's channels that count
-    float s[8];
+  __device__ __forceinline__ float of(const f8 (&v)[K]) const {  // sum of the lane's channels that count
+    float sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) s[c] = counts(k, c) ? v[c] : 0.f;
-    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+    for (int k = 0; k < K; ++k) {
+      float s[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) s[c] = counts(k, c) ? v[k][c] : 0.f;
+      const float all = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+      sum = k ? sum + all : all;
+    }
+    return sum;
   }
-  __device__ __forceinline__ float dot(f8 a, f8 b, int k) const {
+  __device__ __forceinline__ float dot(const f8 (&a)[K], const f8 (&b)[K]) const {
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int c = 0; c < 8; c += 2) {
-      s0 = counts(k, c) ? fmaf(a[c], b[c], s0) : s0;
-      s1 = counts(k, c + 1) ? fmaf(a[c + 1], b[c + 1], s1) : s1;
-    }
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int c = 0; c < 8; c += 2) {
+        s0 = counts(k, c) ? fmaf(a[k][c], b[k][c], s0) : s0;
+        s1 = counts(k, c + 1) ? fmaf(a[k][c + 1], b[k][c + 1], s1) : s1;
+      }
     return s0 + s1;
   }
 
-  // Sums over the entry of every chunk, of one or two values a chunk.  A step of the prefix sum is one instruction: the
+  // Sums over the entry of every lane, of one or two values a lane.  A step of the prefix sum is one instruction: the
   // value of the lane before, times 1 or 0 by whether it belongs to the run.  0 times an infinity or a NaN of another
   // entry would not be 0, so sums that are not finite are taken again with selections (the branch is uniform).  A lane
   // read by DPP has to be written two wait states before, hence the s_nop.
   template <int N>
-  __device__ __forceinline__ void sums(float (&v)[N][K]) const {
-    if constexpr (K == 1) {
-      float s[N];
-      bool fine = true;
+  __device__ __forceinline__ void sums(float (&v)[N]) const {
+    float s[N];
+    bool fine = true;
 #pragma unroll
-      for (int a = 0; a < N; ++a) s[a] = v[a][0];
-      if constexpr (N == 1) {
+    for (int a = 0; a < N; ++a) s[a] = v[a];
+    if constexpr (N == 1) {
 #define SSK_STEP(CTRL) "s_nop 1\n\tv_fmac_f32_dpp %0, %0, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
-        if constexpr (L == 8)
-          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4")
-              : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4));
-        if constexpr (L == 16)
-          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
-              : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
-        if constexpr (L == 32)  // row_bcast:15: lane 15 of the 16 before
-          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
-              SSK_STEP("5 row_bcast:15") : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15));
-        if constexpr (L == 64)  // row_bcast:31: lane 31
-          asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
-              SSK_STEP("5 row_bcast:15") SSK_STEP("6 row_bcast:31")
-              : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15), "v"(m31));
+      if constexpr (L == 8)
+        asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4")
+            : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4));
+      if constexpr (L == 16)
+        asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
+            : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
+      if constexpr (L == 32)  // row_bcast:15: lane 15 of the 16 before
+        asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
+            SSK_STEP("5 row_bcast:15") : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15));
+      if constexpr (L == 64)  // row_bcast:31: lane 31
+        asm(SSK_STEP("1 row_shr:1") SSK_STEP("2 row_shr:2") SSK_STEP("3 row_shr:4") SSK_STEP("4 row_shr:8")
+            SSK_STEP("5 row_bcast:15") SSK_STEP("6 row_bcast:31")
+            : "+v"(s[0]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15), "v"(m31));
 #undef SSK_STEP
-      } else {
+    } else {
 #define SSK_STEP(CTRL)                                                                  \
   "s_nop 1\n\tv_fmac_f32_dpp %0, %0, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t" \
   "v_fmac_f32_dpp %1, %1, %" CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1\n\t"
-        if constexpr (L == 8)
-          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4")
-              : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4));
-        if constexpr (L == 16)
-          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
-              : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
-        if constexpr (L == 32)
-          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
-              SSK_STEP("6 row_bcast:15") : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15));
-        if constexpr (L == 64)
-          asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
-              SSK_STEP("6 row_bcast:15") SSK_STEP("7 row_bcast:31")
-              : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15), "v"(m31));
+      if constexpr (L == 8)
+        asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4")
+            : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4));
+      if constexpr (L == 16)
+        asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
+            : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8));
+      if constexpr (L == 32)
+        asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
+            SSK_STEP("6 row_bcast:15") : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15));
+      if constexpr (L == 64)
+        asm(SSK_STEP("2 row_shr:1") SSK_STEP("3 row_shr:2") SSK_STEP("4 row_shr:4") SSK_STEP("5 row_shr:8")
+            SSK_STEP("6 row_bcast:15") SSK_STEP("7 row_bcast:31")
+            : "+v"(s[0]), "+v"(s[N - 1]) : "v"(m1), "v"(m2), "v"(m4), "v"(m8), "v"(m15), "v"(m31));
 #undef SSK_STEP
-      }
-#pragma unroll
-      for (int a = 0; a < N; ++a) fine = fine && fabsf(s[a]) <= 3.4028235e38f;
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
-#pragma unroll
-        for (int a = 0; a < N; ++a) s[a] = v[a][0];
-#define SSK_STEP(CTRL, M)                              \
-  _Pragma("unroll") for (int a = 0; a < N; ++a) {      \
-    const float o_ = dpp_or_0<CTRL>(s[a]);             \
-    s[a] += (M) != 0.f ? o_ : 0.f;                     \
-  }
-        SSK_STEP(0x111, m1)
-        SSK_STEP(0x112, m2)
-        SSK_STEP(0x114, m4)
-        if constexpr (L >= 16) { SSK_STEP(0x118, m8) }
-        if constexpr (L >= 32) { SSK_STEP(0x142, m15) }
-        if constexpr (L >= 64) { SSK_STEP(0x143, m31) }
-#undef SSK_STEP
-      }
-#pragma unroll
-      for (int a = 0; a < N; ++a) v[a][0] = read_lane(s[a], last);
-    } else {
-      float out[N][K] = {};
-      for (int en = 0; en < n; ++en)
-#pragma unroll
-        for (int a = 0; a < N; ++a) {
-          float s = 0.f;
-#pragma unroll
-          for (int k = 0; k < K; ++k) s += e[k] == en ? v[a][k] : 0.f;
-          const float all = wave_total(s);
-#pragma unroll
-          for (int k = 0; k < K; ++k) out[a][k] = e[k] == en ? all : out[a][k];
-        }
-#pragma unroll
-      for (int a = 0; a < N; ++a)
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[a][k] = out[a][k];
     }
+#pragma unroll
+    for (int a = 0; a < N; ++a) fine = fine && fabsf(s[a]) <= 3.4028235e38f;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
+#pragma unroll
+      for (int a = 0; a < N; ++a) s[a] = v[a];
+#define SSK_STEP(CTRL, M)                              \
+_Pragma("unroll") for (int a = 0; a < N; ++a) {      \
+  const float o_ = dpp_or_0<CTRL>(s[a]);             \
+  s[a] += (M) != 0.f ? o_ : 0.f;                     \
+}
+      SSK_STEP(0x111, m1)
+      SSK_STEP(0x112, m2)
+      SSK_STEP(0x114, m4)
+      if constexpr (L >= 16) { SSK_STEP(0x118, m8) }
+      if constexpr (L >= 32) { SSK_STEP(0x142, m15) }
+      if constexpr (L >= 64) { SSK_STEP(0x143, m31) }
+#undef SSK_STEP
+    }
+#pragma unroll
+    for (int a = 0; a < N; ++a) v[a] = read_lane(s[a], last);
   }
 
   // s / m with one correction step: exact where the quotient is a value of fp32 (a mean that equals one of its
   // values gives a difference of exactly zero, on which a relu turns).
-  __device__ __forceinline__ float over_m(float s, int k) const {
-    const float q = s * rm[k];
-    const float r = fmaf(fmaf(-q, m[k], s), rm[k], q);
+  __device__ __forceinline__ float over_m(float s) const {
+    const float q = s * rm;
+    const float r = fmaf(fmaf(-q, m, s), rm, q);
     return fabsf(q) < 3e38f ? r : q;
   }
 
   // xhat in place of x, whose values are scale times x; r = 1 / sqrt(v + eps).
-  __device__ __forceinline__ void norm(f8 (&x)[K], const float (&scale)[K], float (&r)[K], float eps) const {
-    float mu[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) mu[k] = 0.f;
+  __device__ __forceinline__ void norm(f8 (&x)[K], const float (&scale)[K], float& r, float eps) const {
+    float mu = 0.f;
     if (any_scalar) {
-      float s[1][K];
+      float s[1];
+      if constexpr (K == 1) {
+        s[0] = of(x) * scale[0];
+      } else {
+        f8 v[K];
 #pragma unroll
-      for (int k = 0; k < K; ++k) s[0][k] = of(x[k], k) * scale[k];
+        for (int k = 0; k < K; ++k) v[k] = x[k] * scale[k];
+        s[0] = of(v);
+      }
       sums(s);
-#pragma unroll
-      for (int k = 0; k < K; ++k) mu[k] = scalar[k] ? over_m(s[0][k], k) : 0.f;
+      mu = scalar ? over_m(s[0]) : 0.f;
     }
-    float s[1][K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[k][c] = fmaf(x[k][c], scale[k], -mu[k]);
-      s[0][k] = dot(x[k], x[k], k);
-    }
+      for (int c = 0; c < 8; ++c) x[k][c] = fmaf(x[k][c], scale[k], -mu);
+    float s[1] = {dot(x, x)};
     sums(s);
+    r = __builtin_amdgcn_rsqf(fmaf(s[0], rm, eps));
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      r[k] = __builtin_amdgcn_rsqf(fmaf(s[0][k], rm[k], eps));
-      x[k] *= r[k];
-    }
+    for (int k = 0; k < K; ++k) x[k] *= r;
   }
-  __device__ __forceinline__ void norm(f8 (&x)[K], float (&r)[K], float eps) const {
+  __device__ __forceinline__ void norm(f8 (&x)[K], float& r, float eps) const {
     float one[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) one[k] = 1.f;
@@ -408,20 +385,14 @@ struct Row {
   }
 
   // Gradient behind a norm in place of t = gain * dy, from xhat and r: r t - r mean(t) - xhat r sum(t xhat) / m.
-  __device__ __forceinline__ void norm_back(const f8 (&xhat)[K], const float (&r)[K], f8 (&t)[K]) const {
-    float s[2][K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      s[0][k] = of(t[k], k);
-      s[1][k] = dot(t[k], xhat[k], k);
-    }
+  __device__ __forceinline__ void norm_back(const f8 (&xhat)[K], float r, f8 (&t)[K]) const {
+    float s[2] = {of(t), dot(t, xhat)};
     sums(s);
+    const float rr = r * rm, a = scalar ? s[0] * rr : 0.f, b = s[1] * rr;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const float rr = r[k] * rm[k], a = scalar[k] ? s[0][k] * rr : 0.f, b = s[1][k] * rr;
+    for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int c = 0; c < 8; ++c) t[k][c] = fmaf(t[k][c], r[k], fmaf(-xhat[k][c], b, -a));
-    }
+      for (int c = 0; c < 8; ++c) t[k][c] = fmaf(t[k][c], r, fmaf(-xhat[k][c], b, -a));
   }
 
   // A parameter of `fields` values, one per field, as one per channel of the chunks; ones without it.  Chunks past its
@@ -431,58 +402,29 @@ struct Row {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int c = 0; c < 8; ++c) v[k][c] = p ? p[min(f0[k] + field(k, c), fields - 1)] : 1.f;
+      for (int c = 0; c < 8; ++c) v[k][c] = p ? p[min(f0 + field(k, c), fields - 1)] : 1.f;
   }
 
   // The checkpoint of row r: int8 values at q, exponent bytes at b; of the chunks of the first `entries` entries.
   __device__ __forceinline__ void pack(const f8 (&x)[K], int8_t* q0, uint8_t* b0, int r, int C, int B, int entries,
                                        bool on) const {
-    uint32_t amax[K];
+    uint32_t amax = 0;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      amax[k] = 0;
+    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int c = 0; c < 8; ++c)
-        if (counts(k, c)) amax[k] = max(amax[k], __float_as_uint(x[k][c]) & 0x7fffffffu);
-    }
-    // the chunks of a block lie in up to four neighbouring lanes
-    if constexpr (K == 1) {
-      uint32_t o[3];
+        if (counts(k, c)) amax = max(amax, __float_as_uint(x[k][c]) & 0x7fffffffu);
+    uint32_t o[3] = {};  // the other lanes of the block
 #pragma unroll
-      for (int a = 0; a < 3; ++a) o[a] = (uint32_t)__builtin_amdgcn_ds_bpermute(mate[a], (int)amax[0]);
-      amax[0] = max(max(amax[0], o[0]), max(o[1], o[2]));
-    } else {  // lane i of chunk row k is chunk i + 64 k of the row
-      uint32_t all[K];
-#pragma unroll
-      for (int k = 0; k < K; ++k) all[k] = amax[k];
-#pragma unroll
-      for (int s = -3; s <= 3; ++s) {
-        if (s == 0) continue;
-        uint32_t far[K];
-        int blk_far[K];
-        const int to = (i + s) & 63;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          far[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * to, (int)amax[k]);
-          blk_far[k] = __builtin_amdgcn_ds_bpermute(4 * to, hi[k] ? blk[k] : -1);
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const int kk = k + (i + s < 0 ? -1 : i + s > 63 ? 1 : 0);
-#pragma unroll
-          for (int o = 0; o < K; ++o)
-            if (o == kk && blk_far[o] == blk[k]) all[k] = max(all[k], far[o]);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < K; ++k) amax[k] = all[k];
-    }
+    for (int a = 0; a < M - 1; ++a) o[a] = (uint32_t)__builtin_amdgcn_ds_bpermute(mate[a], (int)amax);
+    amax = max(max(amax, o[0]), max(o[1], o[2]));
+    if (!on || e < 0 || e >= entries) return;
+    const int byte = pack_byte(amax);
+    const float scale = pack_inverse(byte);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (!on || hi[k] == 0 || e[k] >= entries) continue;
+      if (RAG && hi[k] == 0) continue;
       int8_t* q = q0 + (uint32_t)(__umul24(r, C) + start[k]);
-      const int byte = pack_byte(amax[k]);
-      const float scale = pack_inverse(byte);
       // 1.5 2^23 + v has v, rounded to nearest even, in its low bits
       uint32_t w[8];
 #pragma unroll
@@ -501,8 +443,8 @@ struct Row {
         for (int c = 0; c < 8; ++c)
           if (counts(k, c)) q[c] = (int8_t)w[c];
       }
-      if (quad[k] == 0) b0[(uint32_t)(__umul24(r, B) + blk[k])] = (uint8_t)byte;
     }
+    if (first) b0[(uint32_t)(__umul24(r, B) + blk[0])] = (uint8_t)byte;
   }
 };
 
@@ -640,21 +582,24 @@ __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc
 }
 
 // GO_(L, K, RAG) for a table.
-#define SSK_SITE_DISPATCH(t_, GO_)               \
-  do {                                           \
-    const int chunks_ = (t_).t0[(t_).n];         \
-    if ((t_).ragged == 2) SSK_SITE_MODE(GO_, 2); \
-    if ((t_).ragged == 1) SSK_SITE_MODE(GO_, 1); \
-    SSK_SITE_MODE(GO_, 0);                       \
+#define SSK_SITE_DISPATCH(t_, GO_)                                    \
+  do {                                                                \
+    const int lanes_ = site_lanes(t_);                                \
+    if ((t_).K == 4) { /* K = 2 would do without empty chunks */      \
+      if ((t_).ragged == 2) GO_(64, 4, 2);                            \
+      GO_(64, 4, 1);                                                  \
+    }                                                                 \
+    if ((t_).ragged == 2) SSK_SITE_MODE(GO_, (t_).K, lanes_, 2);      \
+    if ((t_).ragged == 1) SSK_SITE_MODE(GO_, (t_).K, lanes_, 1);      \
+    SSK_SITE_MODE(GO_, (t_).K, lanes_, 0);                            \
   } while (0)
-#define SSK_SITE_MODE(GO_, R_)                \
-  do {                                        \
-    if (chunks_ <= 8) GO_(8, 1, R_);          \
-    if (chunks_ <= 16) GO_(16, 1, R_);        \
-    if (chunks_ <= 32) GO_(32, 1, R_);        \
-    if (chunks_ <= 64) GO_(64, 1, R_);        \
-    if (chunks_ <= 128) GO_(64, 2, R_);       \
-    GO_(64, 3, R_);                           \
+#define SSK_SITE_MODE(GO_, K_, lanes_, R_) \
+  do {                                     \
+    if ((K_) == 2) GO_(64, 2, R_);         \
+    if ((lanes_) == 8) GO_(8, 1, R_);      \
+    if ((lanes_) == 16) GO_(16, 1, R_);    \
+    if ((lanes_) == 32) GO_(32, 1, R_);    \
+    GO_(64, 1, R_);                        \
   } while (0)
 
 }  // namespace ssconv

@@ -30,17 +30,17 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
   float least[K];  // a gated value counts above this: relu of the scalars, everything else
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
+    main[k] = w.hi[k] > 0 && w.e < t.n_regular;
     at[k] = main[k] ? w.start[k] : 0;
-    least[k] = w.scalar[k] ? 0.f : -__builtin_inff();
-    if (G && main[k] && w.scalar[k]) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
+    least[k] = w.scalar ? 0.f : -__builtin_inff();
+    if (G && main[k] && w.scalar) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
   }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
   for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
     f8 y[K], h[K];
-    float r[K], sig[R::Q];
+    float r, sig[R::Q];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       y[k] = w.template load<T>((const T*)a.y.data + r0 * S, row, S, k, w.start[k]);
@@ -102,19 +102,19 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
   int at[K], blk[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    main[k] = w.hi[k] > 0 && w.e[k] < t.n_regular;
+    main[k] = w.hi[k] > 0 && w.e < t.n_regular;
     at[k] = main[k] ? w.start[k] : 0;
     blk[k] = main[k] ? w.blk[k] : 0;
     sc[k] = main[k] ? sc[k] * gp[k] : gp[k];
     acc[k] = acc_n[k] = kZero;
-    if (G && main[k] && w.scalar[k]) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
+    if (G && main[k] && w.scalar) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
   }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
   for (int64_t r0 = first_row<R::R>(); r0 < a.n; r0 += step) {
     const bool on = w.sub < a.n - r0;
     const int row = w.row_of(a.n - r0);
     f8 y[K], e[K], h[K], dx[K];
-    float r[K], ys[K], hs[K], sig[R::Q];
+    float r, ys[K], hs[K], sig[R::Q];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       y[k] = w.template load_rows<T, PK>(a.y, r0, row, S, By, k, w.start[k], w.blk[k], ys[k]);
@@ -154,17 +154,20 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
       gates.open(buf, S, sig);
       wave_lds_fence();
     }
+    f8 f[K];  // all of them before a product overwrites what a chunk moved back shares with its neighbour
+#pragma unroll
+    for (int k = 0; k < K; ++k) f[k] = G ? lds_get(w, k, buf) : kOne;
+    if (K > 1) wave_lds_fence();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const f8 f = G ? lds_get(w, k, buf) : kOne;
       f8 prod;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const float u = y[k][c] * gp[k][c];
         prod[c] = e[k][c] * u;
-        e[k][c] *= u > 0.f || !w.scalar[k] ? f[c] : 0.f;
+        e[k][c] *= u > 0.f || !w.scalar ? f[k][c] : 0.f;
       }
-      if (G && main[k] && !w.scalar[k]) lds_put(w, k, buf, prod);
+      if (G && main[k] && !w.scalar) lds_put(w, k, buf, prod);
     }
     if (G) {
       wave_lds_fence();
