@@ -49,6 +49,7 @@ int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t) {
     for (int e = t->n; e <= SSCONV_MAX_ENTRIES; ++e) t->t0[e] = lanes;
     if (lanes <= 64) break;
   }
+  if (t->C < kChunk) t->ragged = 3;
   return SSCONV_OK;
 }
 

@@ -30,7 +30,7 @@ struct SiteTab {
   float m[SSCONV_MAX_ENTRIES], rm[SSCONV_MAX_ENTRIES];  // fields, and 1 / fields
   int C, G;                         // channels without the gates, gates
   int n_regular;                    // entries without the gates'
-  int ragged;                       // 1: some entry is no multiple of 8 K channels, 2: some entry has fewer than 8
+  int ragged;                       // 1: some entry is no multiple of 8 K channels, 2: fewer than 8, 3: the whole row has
 };
 
 // gated: the gates of the fields of order > 0 as one more entry.

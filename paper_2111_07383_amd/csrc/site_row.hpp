@@ -4,9 +4,10 @@
 // Loads and stores are one 16-byte access a chunk (bf16; two in fp32, 8 bytes of a checkpoint) at whatever alignment
 // the row has, so nothing passes through LDS but what lanes owe each other.  RAG = 1: an entry that is no multiple of 8
 // ends in a chunk moved back to its end: its first `lo` channels are the previous chunk's too, take part in no sum and are
-// computed and stored twice, with the same bits.  RAG = 2: entries under 8 channels have one chunk of `hi` channels, moved
-// element by element, which every chunk then has branches for (backward of a tail of 60k rows of 303 channels without
-// narrow entries: 126 us with them, 94 without).
+// computed and stored twice, with the same bits.  RAG = 2: an entry under 8 channels has one chunk, which reads its
+// neighbours' channels too, so that all loads are alike, and stores the entry's element by element (150k rows of 36
+// channels in four entries: backward of a tail 52 us with loads by element, 39 so).  RAG = 3: rows under 8 channels, where
+// that would leave the row: all element by element.
 //
 // An entry begins with a lane, so it is a run of lanes; what its last lane has no chunk for is left empty.  Its sums are
 // a segmented prefix sum (3 to 6 DPP additions, whatever the number of entries) of which the run's last lane is read
@@ -106,6 +107,7 @@ struct Row {
   float m, rm;                      // fields of the entry, and 1 / m
   bool scalar;
   bool any_scalar;                  // uniform
+  bool narrow;                      // the entry has less than 8 channels, all in the first chunk
   bool first;                       // of the lanes of its block
   int last;                         // ds_bpermute address of the last lane of the run
   int mate[3];                      // and of the other lanes of the block
@@ -115,7 +117,7 @@ struct Row {
     const int lane = threadIdx.x & 63;
     i = lane & (L - 1);
     sub = lane / L;
-    any_scalar = scalar = false;
+    any_scalar = scalar = narrow = false;
     int seg0 = i, seg1 = i;  // a lane without an entry is a run of its own
     e = -1;
     f0 = 0;
@@ -137,16 +139,21 @@ struct Row {
       scalar = in ? t.l[en] == 0 : scalar;
       seg0 = in ? t0 : seg0;
       seg1 = in ? t1 - 1 : seg1;
+      if (RAG == 2) narrow = in ? w < 8 : narrow;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int j = (i - t0) * K + k, at = 8 * j;
         const bool here = RAG ? in && at < w : in;
         int s = at, skip = 0, end = 8;
-        if (RAG) {
-          const bool over = at + 8 > w;
-          s = over ? (RAG == 2 ? max(w - 8, 0) : w - 8) : at;
+        if (RAG == 3) {
+          end = w;
+        } else if (RAG == 2 && w < 8) {
+          s = min(0, (en < t.n_regular ? t.C : t.ch0[t.n]) - 8 - ch0);
+          skip = -s;
+          end = skip + w;
+        } else if (RAG) {
+          s = min(at, w - 8);
           skip = at - s;
-          if (RAG == 2) end = min(w, 8);
         }
         start[k] = here ? ch0 + s : start[k];
         rel[k] = here ? s : rel[k];
@@ -170,7 +177,7 @@ struct Row {
   }
 
   __device__ __forceinline__ int field(int k, int v) const {  // of channel v of the chunk, in its entry; < 1024 channels
-    return ((rel[k] + v) * inv) >> 16;
+    return ((RAG == 2 ? max(rel[k] + v, 0) : rel[k] + v) * inv) >> 16;
   }
 
   // Every matrix is addressed from the wavefront's first row (scalar registers) by 32-bit offsets of the lanes.  Rows
@@ -178,13 +185,13 @@ struct Row {
   __device__ __forceinline__ int row_of(int64_t left) const { return min(sub, (int)min(left, (int64_t)R) - 1); }
 
   // The channels of a chunk, of row r of a matrix of C channels, from channel s on (start[k], or 0 where the chunk lies
-  // past a matrix without the gates).  Without narrow entries a lane with no chunk there reads the row's first channels,
-  // which nothing uses; else it has zeros.
+  // past a matrix without the gates).  A lane with no chunk there reads the row's first channels, which nothing
+  // uses; in rows under 8 channels it has zeros.
   template <typename T>
   __device__ __forceinline__ f8 load(const void* p, int r, int C, int k, int s) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
     const T* q = reinterpret_cast<const T*>((const char*)p + (__umul24(r, C) + s) * (uint32_t)sizeof(T));
-    if (RAG < 2 || hi[k] == 8) {
+    if (RAG < 3) {
       v = load8<T>(q);
     } else {
 #pragma unroll
@@ -200,10 +207,10 @@ struct Row {
                                             float& scale) const {
     f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
     scale = 1.f;
-    if (RAG == 2 && hi[k] == 0) return v;
+    if (RAG == 3 && hi[k] == 0) return v;
     const int8_t* at = (const int8_t*)p + (uint32_t)(__umul24(r, C) + s);
     u2 q = {0, 0};
-    if (RAG < 2 || hi[k] == 8) {
+    if (RAG < 3) {
       q = *reinterpret_cast<const u2_any*>(at);
     } else {
 #pragma unroll
@@ -221,7 +228,7 @@ struct Row {
     const float x_lo = pack_scale(b[(uint32_t)(__umul24(r, B) + to_lo)]);
 #pragma unroll
     for (int c = 0; c < 8; ++c) v[c] *= c < lo[k] ? x_lo : x;
-    if (RAG == 2 && hi[k] < 8)  // 0 * NaN
+    if (RAG == 3)  // 0 * NaN
 #pragma unroll
       for (int c = 1; c < 8; ++c)
         if (c >= hi[k]) v[c] = 0.f;
@@ -241,14 +248,17 @@ struct Row {
   template <typename T>
   __device__ __forceinline__ void store(void* p, int r, int C, int k, f8 v) const {
     T* q = reinterpret_cast<T*>((char*)p + (__umul24(r, C) + start[k]) * (uint32_t)sizeof(T));
-    if (RAG < 2 || hi[k] == 8) {
+    if (!by_element(k)) {
       if (hi[k]) store8(q, v);
     } else {
 #pragma unroll
-      for (int c = 0; c < 7; ++c)
-        if (c < hi[k]) q[c] = DT<T>::from_f(v[c]);
+      for (int c = 0; c < 8; ++c)
+        if (counts(k, c)) q[c] = DT<T>::from_f(v[c]);
     }
   }
+
+  // A chunk whose channels are stored one by one.
+  __device__ __forceinline__ bool by_element(int k) const { return RAG == 3 || (RAG == 2 && k == 0 && narrow); }
 
   __device__ __forceinline__ bool counts(int k, int c) const { return !RAG || (c >= lo[k] && (RAG == 1 || c < hi[k])); }
 
@@ -526,17 +536,17 @@ struct Gates {
   }
 };
 
-// 8 channels of a row in LDS; those past hi (where the chunk is no whole one) are left alone.
+// The channels of a chunk in a row in LDS.
 template <int L, int K, int RAG>
 __device__ __forceinline__ void lds_put(const Row<L, K, RAG>& w, int k, float* buf, f8 v) {
   if constexpr (!RAG) {
     *reinterpret_cast<f8*>(buf + w.start[k]) = v;
-  } else if (RAG == 1 || w.hi[k] == 8) {
+  } else if (!w.by_element(k)) {
     *reinterpret_cast<f8_any*>(buf + w.start[k]) = v;
   } else {
 #pragma unroll
-    for (int c = 0; c < 7; ++c)
-      if (c < w.hi[k]) buf[w.start[k] + c] = v[c];
+    for (int c = 0; c < 8; ++c)
+      if (w.counts(k, c)) buf[w.start[k] + c] = v[c];
   }
 }
 template <int L, int K, int RAG>
@@ -585,6 +595,7 @@ __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc
 #define SSK_SITE_DISPATCH(t_, GO_)                                    \
   do {                                                                \
     const int lanes_ = site_lanes(t_);                                \
+    if ((t_).ragged == 3) GO_(8, 1, 3); /* at most 8 entries */       \
     if ((t_).K == 4) { /* K = 2 would do without empty chunks */      \
       if ((t_).ragged == 2) GO_(64, 4, 2);                            \
       GO_(64, 4, 1);                                                  \

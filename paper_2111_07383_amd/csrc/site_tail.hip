@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
     for (int k = 0; k < K; ++k) {
       y[k] = w.template load<T>((const T*)a.y.data + r0 * S, row, S, k, w.start[k]);
       h[k] = kZero;
-      if (RAG < 2 || main[k]) h[k] = w.template load<T>((const T*)a.h.data + r0 * C, row, C, k, at[k]);
+      if (RAG < 3 || main[k]) h[k] = w.template load<T>((const T*)a.h.data + r0 * C, row, C, k, at[k]);
     }
     if (a.yq) w.pack(y, a.yq + r0 * S, a.ye + r0 * By, row, S, By, t.n, on);
     w.norm(y, r, a.eps);
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
       y[k] = w.template load_rows<T, PK>(a.y, r0, row, S, By, k, w.start[k], w.blk[k], ys[k]);
       e[k] = h[k] = dx[k] = kZero;
       hs[k] = 1.f;
-      if (RAG == 2 && !main[k]) continue;
+      if (RAG == 3 && !main[k]) continue;
       e[k] = w.template load<T>((const T*)a.dh + r0 * C, row, C, k, at[k]);
       if (!a.dx) continue;
       dx[k] = w.template load<T>((const T*)a.dx + r0 * C, row, C, k, at[k]);
