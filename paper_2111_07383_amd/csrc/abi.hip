@@ -117,11 +117,11 @@ extern "C" size_t ssconv_backward_workspace_size(ssconv_rulebook_t rb, ssconv_dt
 }
 
 // Checks and runs a backward call.  whole: with the largest tiles of the kernel gradient too, whose sums are in another
-// order; ssconv_backward keeps the order that it has always had.
+// order; ssconv_backward keeps the order that it has always had.  cleared: the split path's words are zero already.
 static int run_backward(const void* feats, const void* grad_out, ssconv_dtype dtype, int cin, int cout,
                         ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc, const float* basis,
                         void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes, bool whole,
-                        hipStream_t stream) {
+                        bool cleared, hipStream_t stream) {
   SSC_TRY(check_conv_args(feats, grad_out, dtype, cin, cout, rb, W));
   SSC_TRY(rulebook_settle(rb));
   if (grad_feats && !aligned16(grad_feats)) return fail(SSCONV_E_INVALID, "grad_feats must be 16-byte aligned");
@@ -153,7 +153,7 @@ static int run_backward(const void* feats, const void* grad_out, ssconv_dtype dt
   const bool fork_tail = both && !L.pair_feats() && rb->n_in > 0 && dtype == SSCONV_F32;
   bool need_join = fork;
   BwdRows rows;
-  if ((grad_coeffs && L.split_rows) || (grad_feats && L.feats == BwdLayout::kSplit))
+  if (!cleared && ((grad_coeffs && L.split_rows) || (grad_feats && L.feats == BwdLayout::kSplit)))
     SSC_TRY(clear_split_flags(SplitFlags{(int*)(ws + L.flags)}, stream));
   if (grad_coeffs) SSC_TRY(bwd_rows(feats, grad_out, dtype, cin, cout, rb, (char*)workspace, L, &rows, stream));
   if (fork) SSC_TRY(aux_fork(stream, &dw_stream));
@@ -189,7 +189,7 @@ extern "C" int ssconv_backward(const void* feats, const void* grad_out, ssconv_d
                                void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes,
                                hipStream_t stream) {
   return run_backward(feats, grad_out, dtype, cin, cout, rb, W, desc, basis, grad_feats, grad_coeffs, workspace,
-                      ws_bytes, false, stream);
+                      ws_bytes, false, false, stream);
 }
 
 // ---------------------------------------------------------------------------
@@ -229,8 +229,13 @@ extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8
   if (rb->n_out > 0 && !grad_out) return fail(SSCONV_E_INVALID, "NULL input buffer");
   void* rows = workspace;
   const size_t used = packed_rows_bytes(rb, dtype, t.C);
-  if (grad_coeffs && rb->n_in > 0)
-    SSC_TRY(expand_packed(t, dtype, q, exps, rb->n_in, norm != 0, (float)eps, gain, rows, stream));
+  const bool expand = grad_coeffs && rb->n_in > 0;
+  if (expand) {
+    const BwdLayout L = bwd_layout(rb, dtype, t.C, cout, true);
+    SplitFlags clear;
+    if (L.split_rows || L.feats == BwdLayout::kSplit) clear.w = (int*)((char*)workspace + used + L.flags);
+    SSC_TRY(expand_packed(t, dtype, q, exps, rb->n_in, norm != 0, (float)eps, gain, rows, clear, stream));
+  }
   return run_backward(rows, grad_out, dtype, t.C, cout, rb, W, desc, basis, grad_feats, grad_coeffs,
-                      (char*)workspace + used, ws_bytes - used, true, stream);
+                      (char*)workspace + used, ws_bytes - used, true, expand, stream);
 }

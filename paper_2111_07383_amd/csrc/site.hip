@@ -169,7 +169,7 @@ extern "C" int ssconv_unpack(const ssconv_fields* fields, const int8_t* q, const
   SSC_TRY(check_site(fields, false, dtype, n, &t));
   if (n == 0) return SSCONV_OK;
   if (!x || !q || !exps) return fail(SSCONV_E_INVALID, "NULL feature or checkpoint buffer");
-  return launch_unpack(t, dtype, q, exps, n, x, stream);
+  return launch_unpack(t, dtype, q, exps, n, x, SplitFlags{}, stream);
 }
 
 extern "C" int ssconv_site_norm_forward(const ssconv_fields* fields, const ssconv_rows* x, ssconv_dtype dtype,

@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "common.hpp"
+#include "split_guard.hpp"
 
 namespace ssconv {
 
@@ -82,6 +83,7 @@ struct NormArgs {
   uint8_t* exps;
   float* part;     // [workgroups][C] (backward); one workgroup writes dgain
   float* dgain;
+  SplitFlags clear;  // words to clear, if any (forward)
 };
 struct TailArgs {
   ssconv_rows y, h;  // h: h_out in the backward
@@ -103,18 +105,20 @@ int launch_tail_fwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStr
 int launch_tail_bwd(const SiteTab& t, ssconv_dtype dt, const TailArgs& a, hipStream_t st);
 int launch_pack(const SiteTab& t, ssconv_dtype dt, const void* x, int64_t n, int8_t* q, uint8_t* exps, hipStream_t st);
 int launch_unpack(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, void* x,
-                  hipStream_t st);
+                  const SplitFlags& clear, hipStream_t st);
 
-// Rows of a checkpoint, or their site norm, for the gradient of a convolution (checked arguments).
+// Rows of a checkpoint, or their site norm, for the gradient of a convolution (checked arguments; n > 0), which also
+// clears that call's words, so that small calls need a launch less.
 inline int expand_packed(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, bool norm,
-                         float eps, const float* gain, void* rows, hipStream_t st) {
-  if (!norm) return launch_unpack(t, dt, q, exps, n, rows, st);
+                         float eps, const float* gain, void* rows, const SplitFlags& clear, hipStream_t st) {
+  if (!norm) return launch_unpack(t, dt, q, exps, n, rows, clear, st);
   NormArgs a{};
   a.x = ssconv_rows{q, exps};
   a.n = n;
   a.eps = eps;
   a.gain = gain;
   a.out = rows;
+  a.clear = clear;
   return launch_norm_fwd(t, dt, a, st);
 }
 

@@ -6,10 +6,15 @@
 namespace ssconv {
 namespace {
 
+__device__ __forceinline__ void clear_words(const SplitFlags& f) {
+  if (f.w && blockIdx.x == 0 && threadIdx.x < SplitFlags::kBytes / 4) f.w[threadIdx.x] = 0;
+}
+
 template <typename T, int L, int K, int RAG, bool PK>
 __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void norm_fwd_kernel(SiteTab t, NormArgs a) {
   using R = Row<L, K, RAG>;
   R w;
+  clear_words(a.clear);
   w.init(t, t.n);
   const int C = t.ch0[t.n], B = t.b0[t.n];
   f8 g[K];
@@ -92,9 +97,10 @@ __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kern
 
 template <typename T, int L, int K, int RAG>
 __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void unpack_kernel(SiteTab t, const int8_t* q, const uint8_t* exps, int64_t n,
-                                                         T* x) {
+                                                         T* x, SplitFlags clear) {
   using R = Row<L, K, RAG>;
   R w;
+  clear_words(clear);
   w.init(t, t.n);
   const int C = t.ch0[t.n], B = t.b0[t.n];
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);
@@ -160,10 +166,10 @@ int launch_pack(const SiteTab& t, ssconv_dtype dt, const void* x, int64_t n, int
 }
 
 int launch_unpack(const SiteTab& t, ssconv_dtype dt, const int8_t* q, const uint8_t* exps, int64_t n, void* x,
-                  hipStream_t st) {
+                  const SplitFlags& clear, hipStream_t st) {
   const unsigned nb = site_blocks(t, n, norm_fwd_per_cu);
   auto go = [&](auto kernel, auto* p) {
-    kernel<<<nb, kSiteNT, 0, st>>>(t, q, exps, n, p);
+    kernel<<<nb, kSiteNT, 0, st>>>(t, q, exps, n, p, clear);
     SSC_HIP(hipGetLastError());
     return (int)SSCONV_OK;
   };
