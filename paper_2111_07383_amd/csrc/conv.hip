@@ -503,12 +503,12 @@ static size_t kgrad_copy_bytes(ssconv_dtype dt, int64_t n, int c) {
 // (the tenth in favour of the ring kernel is what the fit is good for).  Where each row is gathered a few times
 // only the split alone is too much (60 -> 120 channels, 99k pairs of 79k rows: 22 us and 15 for the split against 36
 // on the ring kernel; 17k of 1.9k: 9 and 4 against 20).
-static bool split_kgrad_wins(const ssconv_rulebook* rb, int cin, int cout) {
+static bool split_kgrad_wins(const ssconv_rulebook* rb, int cin, int cout, bool whole) {
   if (rb->n_pairs < 6 * (rb->n_in + rb->n_out)) return false;
   const KgradPlan r = kgrad_plan(rb, SSCONV_F32, cin, cout);
-  const KgradTile t = kgrad_tile(rb, 3, cin, cout, false);
+  const KgradTile t = kgrad_tile(rb, 3, cin, cout, whole);
   const double pairs = (double)rb->n_pairs, partial = 8.0 * cin * cout / 4.5e6;
-  const double r_units = std::max(rb->K, kgrad_f32_units_want(rb, cin, cout)), t_units = std::max(rb->K, t.units);
+  const double r_units = std::max(rb->K, kgrad_f32_units_want(rb, cin, cout, whole)), t_units = std::max(rb->K, t.units);
   const double r_tiles = r.mtiles * r.ntiles, t_tiles = t.mtiles * t.ntiles, B = r.wmb * r.wnb;
   // sums of more pairs than these in one accumulator lose to the tile kernel's, which are rounded once per 32 pairs
   // (60k sites, 5x5x5, 208 -> 208, 8400 pairs a unit: error 1.7e-6 of the result against 0.9e-6, 4138 and 4150 us)
@@ -525,9 +525,9 @@ static bool split_kgrad_wins(const ssconv_rulebook* rb, int cin, int cout) {
 
 // The kernel gradient on the bf16 matrix cores: every row offset below 2^31.  Overrides 6 and 12 keep the
 // other bf16 kernels (12 where it has the channels in columns), 7 the fp32 one that loads rows into registers.
-static bool use_kgrad_tiles(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout) {
+static bool use_kgrad_tiles(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout, bool whole) {
   const int64_t v = debug_gather_variant();
-  if (dt == SSCONV_F32 && v != 13 && !split_kgrad_wins(rb, cin, cout)) return false;
+  if (dt == SSCONV_F32 && v != 13 && !split_kgrad_wins(rb, cin, cout, whole)) return false;
   if (dt == SSCONV_F32 ? v == 7 : v == 6 || (v == 12 && kgrad_supported(dt, cin, cout))) return false;
   // padding bf16 rows is a launch: not where the generic kernel is done sooner, whose time grows with the longest
   // list (3x3x3: 979 pairs, 48 in the longest list, 71 -> 45: 17.5 us against 21.8, 60 -> 120: 18.7 against 22.2;
@@ -553,7 +553,7 @@ static bool use_kgrad_units(const ssconv_rulebook* rb, ssconv_dtype dt, int cin,
 // the wavefront slots.
 static KgradUnits plan_units(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int cout, bool tiles, bool whole) {
   if (dt == SSCONV_F32 && !tiles)
-    return kgrad_units(rb, kgrad_f32_units_want(rb, cin, cout), kKgradMaxUnitsF32);
+    return kgrad_units(rb, kgrad_f32_units_want(rb, cin, cout, whole), kKgradMaxUnitsF32);
   return kgrad_units(rb, kgrad_tile(rb, dt == SSCONV_F32 ? 3 : 1, cin, cout, whole).units, kKgradMaxUnits);
 }
 
@@ -606,7 +606,7 @@ BwdLayout bwd_layout(const ssconv_rulebook* rb, ssconv_dtype dt, int cin, int co
   L.whole = whole;
   const size_t K = rb->K, sz = dtype_bytes(dt);
   size_t nparts;  // fp32 partial tiles of cout x cin
-  L.tiles = use_kgrad_tiles(rb, dt, cin, cout);
+  L.tiles = use_kgrad_tiles(rb, dt, cin, cout, whole);
   if (L.tiles || use_kgrad_units(rb, dt, cin, cout)) {
     L.units = plan_units(rb, dt, cin, cout, L.tiles, whole);
     nparts = (size_t)L.units.nunits;

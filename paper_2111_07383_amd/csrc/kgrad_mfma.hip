@@ -26,6 +26,7 @@
 // base..base+3 of channel c0 + i.  Two such reads form one MFMA operand.  The
 // pair indices of a slice are staged in LDS 1024 at a time.
 #include <algorithm>
+#include <cmath>
 
 #include "kgrad_mfma.hpp"
 #include "lds_dma.hpp"
@@ -567,7 +568,7 @@ bool kgrad_f32_units_ok(const ssconv_rulebook* rb, int cin, int cout) {
          (int64_t)rb->n_in * cin * 4 < ((int64_t)1 << 31) && debug_gather_variant() != 7;
 }
 
-int kgrad_f32_units_want(const ssconv_rulebook* rb, int cin, int cout) {
+int kgrad_f32_units_want(const ssconv_rulebook* rb, int cin, int cout, bool whole) {
   const KgradPlan p = kgrad_plan(rb, SSCONV_F32, cin, cout);
   // one full round of the 2048 wavefront slots (256 CUs x two four-wavefront workgroups): measured
   // against 1024, 1536, 3072 and 4096 tasks, fewer partials to add up outweigh the balance of
@@ -575,7 +576,16 @@ int kgrad_f32_units_want(const ssconv_rulebook* rb, int cin, int cout) {
   const int64_t slots = std::max(1, 2048 / (p.mtiles * p.ntiles));
   // at least ~256 pairs per unit: below that the partial tiles (written once, added up again)
   // outweigh the gathered rows of the unit (C6: 1024 units of ~83 pairs made 35 MB of partials)
-  const int64_t by_pairs = std::max<int64_t>(rb->K, rb->n_pairs / 256);
+  double len = 256;
+  // `whole`: where up to four tiles hold the kernel, the length at which four pairs of a task take as long as the partials they
+  // need (times of split_kgrad_wins), if that is shorter (fp32 gradients from checkpoints with 256 pairs and so: 36 -> 44
+  // channels, 4.9k pairs 54 and 31 us; 32 -> 40, 19k 43 and 27; 71 -> 87, 12k 47 and 35; 52 -> 64, 99k 58 and 49; 104 ->
+  // 128, 19k 50 and 45; in eight and more tiles 208 -> 256, 37k 97 and 86, 12k 66 and 67, 312 -> 384, 37k 154 and 163)
+  if (whole && p.mtiles * p.ntiles <= 4) {
+    const double step = 0.15 + 0.018 * p.wmb * p.wnb, partial = 8.0 * cin * cout / 4.5e6;
+    len = std::min(len, std::max(16.0, std::sqrt(4.0 * rb->n_pairs * partial / step)));
+  }
+  const int64_t by_pairs = std::max<int64_t>(rb->K, (int64_t)(rb->n_pairs / len));
   return (int)std::max<int64_t>(1, std::min(slots, by_pairs));
 }
 

@@ -45,7 +45,7 @@ constexpr int kKgradFoldBlocks = 16, kKgradRingPairs = 2048;
 // fp32 kernel gradient over work units (per-wavefront LDS ring): usable when every row offset
 // fits 31 bits; the unit count that fills one round of wavefront slots.
 bool kgrad_f32_units_ok(const ssconv_rulebook* rb, int cin, int cout);
-int kgrad_f32_units_want(const ssconv_rulebook* rb, int cin, int cout);
+int kgrad_f32_units_want(const ssconv_rulebook* rb, int cin, int cout, bool whole);
 int kgrad_f32(const void* grad_out, const void* feats, int cin, int cout, const ssconv_rulebook* rb,
               const KgradUnits& units, float* part, hipStream_t st, const OnlyIf& only = OnlyIf());
 

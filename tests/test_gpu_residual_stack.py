@@ -128,8 +128,8 @@ def test_checkpoints(dtype):
         dy, dh, dsc, dpo, dne = P.residual_backward(F, y, h, dh, dx, st.scale[i], st.gain_post[i],
                                                     st.gain_pre[i + 1] if i < 2 else None, EPS)
         assert torch.equal(dsc, g["scale"][i]) and torch.equal(dpo, g["gain_post"][i])
-        x = P.site_norm_forward(F, P.pack(F, plain.h[i]), st.gain_pre[i], EPS, dtype=dtype)
-        dx, gc = P.backward(x, dy, L.rb, L.W, L.desc, L.basis)
+        dx, gc = P.backward_packed(P.pack(F, plain.h[i]), dy, L.rb, L.W, L.desc, L.basis, norm=True, gain=st.gain_pre[i],
+                                   eps=EPS)
         assert torch.equal(gc, g["coeffs"][i])
     want, dg = P.site_norm_backward(F, P.pack(F, feats), dx, st.gain_pre[0], EPS, dres=dh)
     assert torch.equal(want, dfeats) and torch.equal(dg, g["gain_pre"][0])
