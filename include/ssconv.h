@@ -397,7 +397,8 @@ int ssconv_unpack(const ssconv_fields* fields /*host*/, const int8_t* q, const u
  * stream, and the normed input of the convolution is not kept at all), in `dtype`.
  * grad_feats is the gradient of that input, before any norm.  The rows are expanded into
  * the workspace (ssconv_backward_packed_workspace_size bytes, 256-byte aligned) where
- * grad_coeffs is asked for.  Everything else, errors too, as ssconv_backward. */
+ * grad_coeffs is asked for.  Everything else, errors too, as ssconv_backward, of which
+ * grad_coeffs may differ in the order of its fp32 sums. */
 size_t ssconv_backward_packed_workspace_size(ssconv_rulebook_t rb, ssconv_dtype dtype, int cin, int cout);
 int ssconv_backward_packed(const ssconv_fields* fields_in /*host*/, const int8_t* q, const uint8_t* exps, int norm,
                            double eps, const float* gain, const void* grad_out, ssconv_dtype dtype, int cout,

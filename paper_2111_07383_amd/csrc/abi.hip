@@ -117,7 +117,8 @@ extern "C" size_t ssconv_backward_workspace_size(ssconv_rulebook_t rb, ssconv_dt
 }
 
 // Checks and runs a backward call.  whole: with the largest tiles of the kernel gradient and its shortest work units
-// too, whose sums are in another order; ssconv_backward keeps the order that it has always had.  cleared: the split path's words are zero already.
+// too, whose sums are in another order; ssconv_backward keeps the order that it has always had.  cleared: the split
+// path's words are zero already.
 static int run_backward(const void* feats, const void* grad_out, ssconv_dtype dtype, int cin, int cout,
                         ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc, const float* basis,
                         void* grad_feats, float* grad_coeffs, void* workspace, size_t ws_bytes, bool whole,

@@ -53,8 +53,8 @@ inline int site_rows(const SiteTab& t) { return kSiteNT / site_lanes(t); }
 // Workgroups of a compute unit at a time, by a kernel's registers (their launch bounds); a workgroup is one wavefront
 // per SIMD.  All loop over the rows, so a grid of more would run in rounds of which the last is part empty (backward of
 // a 208-channel tail: 1024 workgroups of 144 registers, of which 768 fit, 235 us; the next version, 1024 of 128
-// registers, 127).  The norm's backward would hold 8; its partial sums then cost more (191.8k rows of 208 channels forward and
-// backward with 8 97 us, 6 94, 4 101).  Backward of a tail of 60k rows of 312 channels: 3 85 us, 4 73.
+// registers, 127).  The norm's backward would hold 8; its partial sums then cost more (191.8k rows of 208 channels
+// forward and backward with 8 97 us, 6 94, 4 101).  Backward of a tail of 60k rows of 312 channels: 3 85 us, 4 73.
 constexpr int norm_fwd_per_cu(int L, int K, int rag) { return K == 4 ? 2 : K == 2 || rag ? 5 : 8; }
 constexpr int norm_bwd_per_cu(int L, int K, int rag) { return K == 4 ? 1 : K == 2 ? 3 : rag || L == 64 ? 5 : 6; }
 constexpr int tail_fwd_per_cu(int L, int K, int rag) { return K == 4 ? 1 : K == 2 ? 3 : rag ? 4 : L == 64 ? 5 : 6; }

@@ -79,7 +79,8 @@ __global__ __launch_bounds__(kSiteNT, norm_bwd_per_cu(L, K, RAG)) void norm_bwd_
 }
 
 template <typename T, int L, int K, int RAG>
-__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kernel(SiteTab t, const T* x, int64_t n, int8_t* q, uint8_t* exps) {
+__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kernel(SiteTab t, const T* x, int64_t n,
+                                                                                   int8_t* q, uint8_t* exps) {
   using R = Row<L, K, RAG>;
   R w;
   w.init(t, t.n);
@@ -96,8 +97,9 @@ __global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void pack_kern
 }
 
 template <typename T, int L, int K, int RAG>
-__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void unpack_kernel(SiteTab t, const int8_t* q, const uint8_t* exps, int64_t n,
-                                                         T* x, SplitFlags clear) {
+__global__ __launch_bounds__(kSiteNT, norm_fwd_per_cu(L, K, RAG)) void unpack_kernel(SiteTab t, const int8_t* q,
+                                                                                     const uint8_t* exps, int64_t n, T* x,
+                                                                                     SplitFlags clear) {
   using R = Row<L, K, RAG>;
   R w;
   clear_words(clear);

@@ -503,7 +503,8 @@ struct Gates {
       for (int q = 0; q < Q; ++q) v[q] = p[f0[q]];
   }
 
-  // buf[channel], of a row that ends at `end`: from the gates' inputs in their channels, their sigmoids in all components of what they gate.
+  // buf[channel], of a row that ends at `end`: from the gates' inputs in their channels, their sigmoids in all components
+  // of what they gate.
   __device__ __forceinline__ void open(float* buf, int end, float (&s)[Q]) const {
 #pragma unroll
     for (int q = 0; q < Q; ++q) s[q] = buf[min(at[q], end)];
