@@ -317,7 +317,7 @@ def test_many_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("name", ["ragged", "f104", "w400"])
+@pytest.mark.parametrize("name", ["ragged", "f104", "w400", "gate1", "tiny", "order4", "f36", "narrow64", "w900", "narrow192"])
 def test_views_off_alignment(name, dtype):
     """Buffers that start at any element give the same bits, and nothing outside them is written."""
     f = FIELDS[name]
@@ -355,8 +355,9 @@ def test_views_off_alignment(name, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_in_place(dtype):
-    f, n = FIELDS["ragged"], 300
+@pytest.mark.parametrize("name", ["ragged", "gate1", "order4", "f36", "narrow64", "narrow192"])
+def test_in_place(name, dtype):
+    f, n = FIELDS[name], 300
     full = os_.gate_fields(f)
     C, S, rng = channels(f), channels(full), np.random.default_rng(11)
     x, dy, dres = (dev(values(rng, n, C, dtype), dtype) for _ in range(3))
@@ -407,6 +408,63 @@ def test_non_finite_and_zero_rows(dtype):
     dh[4, 0] = float("inf")
     c = P.residual_backward(f, clean[2], clean[3], dh, dx, eps=EPS)
     assert torch.equal(c[0][rows[5:]], a[0][rows[5:]])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", ["seven", "order4", "tiny", "f36", "ragged", "narrow64", "narrow192", "w900"])
+def test_non_finite_stays_in_its_entry(name, dtype):
+    """Chunks read channels of neighbouring entries: with a NaN in one entry of every row, the others keep their bits."""
+    f, n = FIELDS[name], 11
+    C, rng = channels(f), np.random.default_rng(13)
+    x, d = values(rng, n, C, dtype), values(rng, n, C, dtype)
+    gain = dev(params(rng, f))
+    ref = P.site_norm_forward(f, dev(x, dtype), gain, EPS, checkpoint=True)
+    back = P.site_norm_backward(f, dev(x, dtype), dev(d, dtype), gain, EPS)
+    packed = P.site_norm_backward(f, ref[1], dev(d, dtype), gain, EPS)
+    ch = f0 = 0
+    for l, m in f:
+        w = m * (2 * l + 1)
+        for at, v in ((ch, np.nan), (ch + w - 1, np.inf)):
+            bad = x.copy()
+            bad[:, at] = v
+            got = P.site_norm_forward(f, dev(bad, dtype), gain, EPS, checkpoint=True)
+            keep = [c for c in range(C) if not ch <= c < ch + w]
+            assert bool(torch.isnan(got[0][:, at]).all())
+            assert torch.equal(got[0][:, keep], ref[0][:, keep]) and torch.equal(got[1].q[:, keep], ref[1].q[:, keep])
+            fields = [i for i in range(sum(m for _, m in f)) if not f0 <= i < f0 + m]
+            for u, v in ((P.site_norm_backward(f, dev(bad, dtype), dev(d, dtype), gain, EPS), back),
+                         (P.site_norm_backward(f, got[1], dev(d, dtype), gain, EPS), packed)):
+                assert torch.equal(u[0][:, keep], v[0][:, keep]) and torch.equal(u[1][fields], v[1][fields])
+                assert bool(torch.isnan(u[0][:, at]).all())
+        ch, f0 = ch + w, f0 + m
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", ["order4", "tiny", "f36", "ragged", "narrow64", "narrow192", "w900"])
+def test_non_finite_tail_stays_in_its_entry(name, dtype):
+    """The same of the tail: a NaN in one entry of the stream, of the convolution output or of a gradient."""
+    f, n = FIELDS[name], 11
+    full = os_.gate_fields(f)
+    C, S, rng = channels(f), channels(full), np.random.default_rng(14)
+    y, h, dh, dx = (values(rng, n, c, dtype) for c in (S, C, C, C))
+    run = lambda y, h, dh: (P.residual_forward(f, dev(y, dtype), dev(h, dtype), eps=EPS)[:2] +  # noqa: E731
+                            P.residual_backward(f, dev(y, dtype), dev(h, dtype), dev(dh, dtype), dev(dx, dtype), eps=EPS)[:2])
+    ref = run(y, h, dh)
+    gates = list(range(C, S))
+    ch = 0
+    for l, m in f:
+        w = m * (2 * l + 1)
+        keep = [c for c in range(C) if not ch <= c < ch + w]
+        for which in range(3):
+            bad = [y.copy(), h.copy(), dh.copy()]
+            bad[which][:, ch + w - 1] = np.nan
+            got = run(*bad)
+            for g, r in zip(got[:2] if which < 2 else (), ref[:2]):
+                assert torch.equal(g[:, keep], r[:, keep]) and bool(torch.isnan(g[:, ch + w - 1]).all())
+            for g, r in zip(got[2:], ref[2:]):
+                k = keep if l else keep + (gates if g.shape[1] == S else [])  # a field's gate sees its field
+                assert torch.equal(g[:, k], r[:, k])
+        ch += w
 
 
 def test_empty():
