@@ -142,6 +142,36 @@ def test_backward_packed(name, norm):
     rb.close()
 
 
+@pytest.mark.parametrize("norm", [False, True])
+def test_backward_packed_again_in_one_workspace(norm):
+    """A call leaves nothing behind that the next one in the same workspace sees: between calls whose fp32 rows split into
+    three bf16 parts, ones whose gradients (3e38, infinity) do not."""
+    f, grid = ((0, 16), (1, 16), (2, 8)), 24
+    rng = np.random.default_rng(21)
+    coords = random_sites(rng, 9000, grid)
+    n, C, fo = len(coords), channels(f), gate_fields(f)
+    spec = LayerSpec(3, 1, True, f, fo, shells=(0.0, 1.0), gated=True)
+    desc = P.layer_desc(spec)
+    basis = torch.from_numpy(P.basis_build(desc)).to(DEV)
+    rb = P.Rulebook(torch.from_numpy(coords).to(DEV), grid, 3, 1, True)
+    W = P.synth_kernel(desc, basis, dev(rng.standard_normal(oc.Layer(spec).n_coeff) / 60), torch.float32)
+    p = P.pack(f, dev(rng.standard_normal((n, C)).astype(np.float32)))
+    g = dev(rng.standard_normal((n, spec.cout)).astype(np.float32))
+    ws = torch.full((P.backward_packed_workspace_size(rb, torch.float32, C, spec.cout),), 255, dtype=torch.uint8, device=DEV)
+    kw = dict(norm=norm, eps=1e-5, workspace=ws)
+    ref = P.backward_packed(p, g, rb, W, desc, basis, **kw)
+    for v in (3e38, float("inf")):
+        bad = g.clone()
+        bad[5, 7] = v
+        gf, gc = P.backward_packed(p, bad, rb, W, desc, basis, **kw)
+        assert not torch.equal(gc, ref[1])
+        for need in ({}, {"need_feats": False}, {"need_coeffs": False}):
+            got = P.backward_packed(p, g, rb, W, desc, basis, **need, **kw)
+            for a, b in zip(got, ref):
+                assert a is None or torch.equal(a, b)
+    rb.close()
+
+
 def test_backward_packed_no_sites():
     f = ((0, 2), (1, 1))
     spec = LayerSpec(3, 1, True, f, gate_fields(f), shells=(0.0, 1.0))
