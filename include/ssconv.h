@@ -379,11 +379,13 @@ int ssconv_residual_backward(const ssconv_fields* fields /*host*/, const ssconv_
  * blocks start anew with every entry of `fields` (so no block mixes orders) and an
  * entry's last one may be shorter: exps [n, ssconv_packed_blocks(fields)].
  * With amax = a 2^E the block's largest magnitude, 1 <= a < 2:
- *   k = max(-126, E - 6 + (a > 127/64)),  q = round to nearest even of x 2^-k,
- *   byte = k + 127, and q 2^k is the value that is read back (exact in bf16 too).
- * |x - q 2^k| <= 2^(k-1) <= amax / 127 (and 2^-127 where k = -126).  A block with an infinity
- * or a NaN has the byte 255 and reads back as NaN.  A checkpoint of 208 channels
- * in bf16 takes 52% of its memory, in fp32 26%.
+ *   k = max(-126, min(121, E - 6 + (a > 127/64))),
+ *   q = round to nearest even of x 2^-k, held to -127..127 (k = 121 alone needs it),
+ *   byte = k + 127, and q 2^k is the value that is read back (exact in bf16 too, and
+ * finite).  |x - q 2^k| <= 2^(k-1) <= amax / 127 (2^-127 where k = -126); values beyond
+ * 127 2^121 = 3.376e38 are read back as that, which is off by less than amax / 127.  A
+ * block with an infinity or a NaN has the byte 255 and reads back as NaN.  A checkpoint
+ * of 208 channels in bf16 takes 52% of its memory, in fp32 26%.
  * C = 1..1024.  n = 0 is a no-op.  Buffers need the alignment of their elements. */
 int64_t ssconv_packed_blocks(const ssconv_fields* fields /*host*/); /* 0 for a bad list */
 int ssconv_pack(const ssconv_fields* fields /*host*/, const void* x, ssconv_dtype dtype, int64_t n, int8_t* q,

@@ -121,8 +121,8 @@ def pack(fields, x):
             amax = np.abs(f).max(1)
             mant, e = np.frexp(amax)                       # amax = mant 2^e, 1/2 <= mant < 1
             k = np.where(amax > 0, e - 7 + (mant > 127 / 128), -126)
-            k = np.maximum(k, -126)
-            qs.append(np.rint(np.ldexp(f, -k[:, None])).astype(np.int8))
+            k = np.clip(k, -126, 121)                      # at 122 the largest values would be 64 2^122 = 2^128
+            qs.append(np.clip(np.rint(np.ldexp(f, -k[:, None])), -127, 127).astype(np.int8))
             es.append(np.where(bad, 255, k + 127).astype(np.uint8))
     return np.concatenate(qs, 1), np.stack(es, 1)
 

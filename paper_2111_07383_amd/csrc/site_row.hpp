@@ -27,10 +27,26 @@ typedef u4 u4_any __attribute__((aligned(2)));
 typedef f8 f8_any __attribute__((aligned(4)));
 typedef u2 u2_any __attribute__((aligned(1)));
 
-// Exponent byte of a block with this largest magnitude (as bits), and its scale and the scale's inverse.
+// Exponent byte of a block with this largest magnitude (as bits), and its scale and the scale's inverse.  At the types'
+// end k stays 121: at 122 the values above 127 2^121 would be 64 2^122 = 2^128, which is infinity.  They are 127 2^121
+// instead, less than 2^121 away, and that is under amax / 127 like everywhere.
+constexpr int kPackTop = 121 + 127;
 __device__ __forceinline__ int pack_byte(uint32_t amax_bits) {
-  const int k = (int)(amax_bits >> 23) - 127 - 6 + ((amax_bits & 0x7fffffu) > 0x7e0000u ? 1 : 0);  // 127/64 = 1 + 63/64
-  return amax_bits >= 0x7f800000u ? 255 : (k < -126 ? -126 : k) + 127;
+  const int byte = (int)(amax_bits >> 23) - 6 + ((amax_bits & 0x7fffffu) > 0x7e0000u ? 1 : 0);  // 127/64 = 1 + 63/64
+  return amax_bits >= 0x7f800000u ? 255 : min(max(byte, 1), kPackTop);
+}
+__device__ __forceinline__ float pack_hold(float x) {  // to -127 2^121 .. 127 2^121
+  return __builtin_amdgcn_fmed3f(x, -0x1.fcp127f, 0x1.fcp127f);
+}
+__device__ __forceinline__ u2 low_bytes(const uint32_t (&w)[8]) {
+  u2 p;
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    const uint32_t l16 = __builtin_amdgcn_perm(w[4 * a + 1], w[4 * a], 0x0c0c0400u);
+    const uint32_t h16 = __builtin_amdgcn_perm(w[4 * a + 3], w[4 * a + 2], 0x04000c0cu);
+    p[a] = l16 | h16;
+  }
+  return p;
 }
 __device__ __forceinline__ float pack_scale(int byte) {
   return __uint_as_float(byte == 255 ? 0x7fc00000u : (uint32_t)byte << 23);
@@ -440,18 +456,18 @@ _Pragma("unroll") for (int a = 0; a < N; ++a) {      \
 #pragma unroll
       for (int c = 0; c < 8; ++c) w[c] = byte == 255 ? 0u : __float_as_uint(fmaf(x[k][c], scale, 12582912.f));
       if (!RAG || (lo[k] == 0 && hi[k] == 8)) {
-        u2 p;
+        u2 p = low_bytes(w);
+        if (__builtin_expect(byte == kPackTop, 0)) {  // taken again from held values: a clamp of w would keep all of it
+          uint32_t held[8];
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const uint32_t l16 = __builtin_amdgcn_perm(w[4 * a + 1], w[4 * a], 0x0c0c0400u);
-          const uint32_t h16 = __builtin_amdgcn_perm(w[4 * a + 3], w[4 * a + 2], 0x04000c0cu);
-          p[a] = l16 | h16;
+          for (int c = 0; c < 8; ++c) held[c] = __float_as_uint(fmaf(pack_hold(x[k][c]), scale, 12582912.f));
+          p = low_bytes(held);
         }
         *reinterpret_cast<u2_any*>(q) = p;
       } else {
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-          if (counts(k, c)) q[c] = (int8_t)w[c];
+          if (counts(k, c)) q[c] = (int8_t)(byte == 255 ? 0u : __float_as_uint(fmaf(pack_hold(x[k][c]), scale, 12582912.f)));
       }
     }
     if (first) b0[(uint32_t)(__umul24(r, B) + blk[0])] = (uint8_t)byte;

@@ -1,0 +1,68 @@
+"""The site norm, the residual tail and the checkpoints where their values and their sums are at an end: the largest finite
+values, infinite gains, sums that cancel, entries that the norm makes zero, gradients that a closed relu stops."""
+import numpy as np
+import pytest
+
+from oracle import site as os_
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+P = pytest.importorskip("paper_2111_07383_amd")
+
+DEV = "cuda:0"
+EPS = 1e-5
+DTYPES = [torch.float32, torch.bfloat16]
+# whole chunks of 8 channels, ragged ones, entries under 8, rows under 8, two and four chunks a lane
+FIELDS = {
+    "f104": ((0, 16), (1, 16), (2, 8)),
+    "ragged": ((0, 13), (1, 11), (2, 5)),
+    "f36": ((0, 4), (1, 4), (2, 4)),
+    "tiny": ((0, 2), (1, 1)),
+    "w900": ((0, 500), (1, 100), (2, 10)),
+    "narrow192": ((0, 3), (0, 770), (1, 60), (2, 1)),
+}
+
+
+def channels(f):
+    return sum(m * (2 * l + 1) for l, m in f)
+
+
+def count(f):
+    return sum(m for _, m in f)
+
+
+def dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(DEV, dtype)
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", list(FIELDS))
+def test_checkpoints_of_the_largest_values(name, dtype):
+    """Finite values are read back finite, up to the types' largest, from every call that writes a checkpoint."""
+    f = FIELDS[name]
+    full = os_.gate_fields(f)
+    rng = np.random.default_rng(1)
+    for fl in (f, full):
+        C, top = channels(fl), torch.finfo(dtype).max
+        x = torch.from_numpy(rng.uniform(-1, 1, (12, C)) * top).to(dtype).to(DEV)
+        x[0], x[1], x[2, -1], x[3, 0], x[4, C // 2] = top, -top, top, -top, top
+        x[5:9] = x[5:9] * 0.997                                     # around 127 2^121, the last that needs no other scale
+        q, e = os_.pack(fl, host(x))
+        want = os_.unpack(fl, q, e)
+        assert np.abs(want).max() <= torch.finfo(torch.bfloat16).max
+        kept = [P.pack(fl, x), P.site_norm_forward(fl, x, checkpoint=True)[1]]
+        if fl == full:
+            h = torch.zeros((12, channels(f)), dtype=dtype, device=DEV)
+            kept.append(P.residual_forward(f, x, h, checkpoint=True)[2])
+        else:
+            y = torch.zeros((12, channels(full)), dtype=dtype, device=DEV)
+            kept.append(P.residual_forward(f, y, x, checkpoint=True)[3])   # a zero y adds nothing to the stream
+        for p in kept:
+            assert np.array_equal(p.q.cpu().numpy(), q) and np.array_equal(p.exps.cpu().numpy(), e)
+            for t in DTYPES:
+                assert np.array_equal(host(P.unpack(p, t)), want)
