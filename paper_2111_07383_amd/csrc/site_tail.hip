@@ -27,12 +27,12 @@ __global__ __launch_bounds__(kSiteNT, tail_fwd_per_cu(L, K, RAG)) void tail_fwd_
   w.params(a.gain_next, gn, t.f0[t.n_regular]);
   bool main[K];  // a chunk of the fields, not of the gates
   int at[K];     // its place in a matrix without the gates
-  float least[K];  // a gated value counts above this: relu of the scalars, everything else
+  float least[K];  // what is at most this becomes 0: relu of the scalars; nothing is at most NaN
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     main[k] = w.hi[k] > 0 && w.e < t.n_regular;
     at[k] = main[k] ? w.start[k] : 0;
-    least[k] = w.scalar ? 0.f : -__builtin_inff();
+    least[k] = w.scalar ? 0.f : __builtin_nanf("");
     if (G && main[k] && w.scalar) lds_put(w, k, buf, kOne);  // a scalar's factor, which nothing overwrites
   }
   const int64_t step = (int64_t)gridDim.x * (kSiteNT / L);

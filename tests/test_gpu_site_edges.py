@@ -66,3 +66,25 @@ def test_checkpoints_of_the_largest_values(name, dtype):
             assert np.array_equal(p.q.cpu().numpy(), q) and np.array_equal(p.exps.cpu().numpy(), e)
             for t in DTYPES:
                 assert np.array_equal(host(P.unpack(p, t)), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", list(FIELDS))
+def test_infinite_components(name, dtype):
+    """A component that a gain takes to an infinity of either sign stays one behind its gate."""
+    f = FIELDS[name]
+    full = os_.gate_fields(f)
+    n, rng = 21, np.random.default_rng(2)
+    y, h = dev(rng.standard_normal((n, channels(full))), dtype), dev(rng.standard_normal((n, channels(f))), dtype)
+    gain = (1 + 0.3 * rng.standard_normal(count(full))).astype(np.float32)
+    ref = P.residual_forward(f, y, h, gain_post=dev(gain), eps=EPS, next_norm=False)[0]
+    hit, at = np.zeros(channels(f), bool), 0
+    for c, first, m, d in os_.entries(f):
+        if d > 1:   # the first and the last field of every entry
+            gain[first], gain[first + m - 1] = np.inf, -np.inf
+            hit[c:c + d] = hit[c + (m - 1) * d:c + m * d] = True
+    got = P.residual_forward(f, y, h, gain_post=dev(gain), eps=EPS, next_norm=False)[0]
+    want = os_.residual_forward(f, host(y), host(h), None, gain, EPS)
+    assert np.isneginf(want[:, hit]).any() and np.isposinf(want[:, hit]).any() and not np.isfinite(want[:, hit]).any()
+    assert np.array_equal(host(got)[:, hit], want[:, hit])
+    assert torch.equal(got[:, torch.from_numpy(~hit)], ref[:, torch.from_numpy(~hit)])
