@@ -154,10 +154,13 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
       gates.open(buf, S, sig);
       wave_lds_fence();
     }
-    f8 f[K];  // all of them before a product overwrites what a chunk moved back shares with its neighbour
+    // All factors are read before the first product is written: a chunk moved back shares channels with its neighbour,
+    // which is another lane's where a lane has one chunk, and no lane's own addresses keep the compiler from starting a
+    // lane's writes between its reads.  Chunks that are whole share nothing with another lane's.
+    f8 f[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) f[k] = G ? lds_get(w, k, buf) : kOne;
-    if (K > 1) wave_lds_fence();
+    if (K > 1 || RAG) wave_lds_fence();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       f8 prod;
