@@ -317,8 +317,9 @@ int ssconv_forward_norm(const void* feats, ssconv_dtype dtype, int cin, ssconv_r
  * not a checkpoint.
  * Backward: dx = the gradient with respect to x of <y, dy>, plus dres (NULL: 0),
  * the gradient that reaches x past the norm; dgain fp32 [fields] (NULL: skipped)
- * = sum over rows of dy * y / gain, in a fixed order (deterministic).  dx may be
- * dy's or dres's buffer.  workspace: device scratch of at least
+ * = sum over rows of dy * y / gain, in a fixed order (deterministic): fp32 over the
+ * rows that a lane takes in turn (6 to 200 of 200k), one rounding of every workgroup's
+ * sum, 64 bits otherwise.  dx may be dy's or dres's buffer.  workspace: device scratch of at least
  * ssconv_site_norm_workspace_size bytes (0 for a few rows), 256-byte aligned, needed
  * where dgain is given; calls that overlap in time need their own.
  * n = 0: dgain becomes 0, nothing else is written.  Nothing is allocated and the
@@ -359,7 +360,7 @@ int ssconv_site_norm_backward(const ssconv_fields* fields /*host*/, const ssconv
  * h_out and dx [n, C] = gradient of x_out (NULL where there was none; h_out may then
  * be NULL): dy [n, C + G], dh_in [n, C] = gradient of h, and dgain_post, dscale,
  * dgain_next (fp32, each NULL to skip; dgain_next NULL without dx), summed over the
- * rows in a fixed order.  relu'(0) = 0.  dh_in may be dh's or dx's buffer.
+ * rows as the norm's dgain.  relu'(0) = 0.  dh_in may be dh's or dx's buffer.
  * workspace: as for the norm, ssconv_residual_workspace_size bytes, needed where
  * one of the three is given.  n = 0, alignment, overlap and errors as for the norm. */
 int ssconv_residual_forward(const ssconv_fields* fields /*host*/, const void* y, const void* h, ssconv_dtype dtype,

@@ -573,8 +573,11 @@ __device__ __forceinline__ f8 lds_get(const Row<L, K, RAG>& w, int k, const floa
 }
 
 // Sums of a per-channel value over the rows that the workgroup's lanes have taken, in a fixed order; lds holds one row of
-// floats per row that the workgroup takes at a time.  All threads call it.  part: to part[channels]; else (the only
-// workgroup of its call) to grad, summed over the components of the fields of `entries` entries.
+// floats per row that the workgroup takes at a time.  All threads call it.  part: to part[channels], for a second launch
+// that adds the workgroups up; else (the only workgroup of its call) to grad, summed over the components of the fields of
+// `entries` entries.  A lane has added the rows that it took in fp32 (of 200k rows 6 on 8 lanes, 24 on 32, 200 where a
+// compute unit holds one workgroup of four rows): 64 bits there would take eight registers more a chunk, which the kernels
+// do not have.  From here on sums are in fp64; a workgroup's is rounded once more, to its partial.
 template <int L, int K, int RAG>
 __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc)[K], int channels, float* lds,
                                          float* part, const SiteTab& t, int entries, float* grad) {
@@ -588,22 +591,27 @@ __device__ __forceinline__ void sum_rows(const Row<L, K, RAG>& w, const f8 (&acc
       if (w.hi[k] > 0 && w.counts(k, c) && w.start[k] + c < channels) mine[w.start[k] + c] = acc[k][c];
   __syncthreads();
   for (int c = threadIdx.x; c < channels; c += kSiteNT) {
-    float s = 0.f;
+    double s = 0.0;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) s += lds[r * channels + c];
-    if (part)
-      part[c] = s;
-    else
-      lds[c] = s;  // its column is this thread's
+    for (int r = 0; r < ROWS; ++r) s += (double)lds[r * channels + c];
+    if (part) {
+      part[c] = (float)s;
+    } else {  // its column is this thread's: the halves of s take the first two rows of it
+      lds[c] = __int_as_float(__double2hiint(s));
+      lds[channels + c] = __int_as_float(__double2loint(s));
+    }
   }
   if (part || !grad) return;
   __syncthreads();
   for (int e = 0; e < entries; ++e) {
     const int d = 2 * t.l[e] + 1;
     for (int f = threadIdx.x; f < t.mult[e]; f += kSiteNT) {
-      float s = 0.f;
-      for (int i = 0; i < d; ++i) s += lds[t.ch0[e] + f * d + i];
-      grad[t.f0[e] + f] = s;
+      double s = 0.0;
+      for (int i = 0; i < d; ++i) {
+        const float* at = lds + t.ch0[e] + f * d + i;
+        s += __hiloint2double(__float_as_int(at[0]), __float_as_int(at[channels]));
+      }
+      grad[t.f0[e] + f] = (float)s;
     }
   }
 }

@@ -88,3 +88,29 @@ def test_infinite_components(name, dtype):
     assert np.isneginf(want[:, hit]).any() and np.isposinf(want[:, hit]).any() and not np.isfinite(want[:, hit]).any()
     assert np.array_equal(host(got)[:, hit], want[:, hit])
     assert torch.equal(got[:, torch.from_numpy(~hit)], ref[:, torch.from_numpy(~hit)])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [3, 150])
+@pytest.mark.parametrize("name", list(FIELDS))
+def test_parameter_sums_that_cancel(name, n, dtype):
+    """Rows of a workgroup and components of a field are added up in 64 bits: three equal rows whose gradients are 2^20, 1
+    and -2^20 times the same (exact in either type) give the parameters' gradients of the one in the middle, to the bit
+    (24 + 20 bits and a few components; in 32 bits 2^-4 of a product would be lost).  n = 3: one workgroup, which writes
+    the gradients itself; 150: partial sums of several, of which the first holds the three."""
+    f = FIELDS[name]
+    full = os_.gate_fields(f)
+    C, S, rng = channels(f), channels(full), np.random.default_rng(3)
+    y, h, dh, dx = (dev(rng.standard_normal((1, c)), dtype) for c in (S, C, C, C))
+    sc, gp, gn = (dev(1 + 0.3 * rng.standard_normal(count(k))) for k in (f, full, f))
+    times = torch.zeros((n, 1), dtype=dtype, device=DEV)
+    times[:3, 0] = torch.tensor([2.0 ** 20, 1, -2.0 ** 20])
+    many = lambda t: t.repeat(n, 1)  # noqa: E731
+    one = P.site_norm_backward(f, h, dx, gn, EPS)[1]
+    assert torch.equal(P.site_norm_backward(f, many(h), times * dx, gn, EPS)[1], one)
+    want = P.residual_backward(f, y, h, dh, dx, sc, gp, gn, EPS)
+    got = P.residual_backward(f, many(y), many(h), times * dh, times * dx, sc, gp, gn, EPS)
+    packed = P.residual_backward(f, P.pack(full, many(y)), P.pack(f, many(h)), times * dh, times * dx, sc, gp, gn, EPS)
+    alone = P.residual_backward(f, P.pack(full, y), P.pack(f, h), dh, dx, sc, gp, gn, EPS)
+    for k in (2, 3, 4):
+        assert torch.equal(got[k], want[k]) and torch.equal(packed[k], alone[k])
