@@ -423,12 +423,14 @@ _Pragma("unroll") for (int a = 0; a < N; ++a) {      \
 
   // A parameter of `fields` values, one per field, as one per channel of the chunks; ones without it.  Chunks past its
   // fields (the gates of a parameter of the fields) get its last value: looking at them here would wait for the loads,
-  // which the first row's overlap.
+  // which the first row's overlap.  0 for an entry of one scalar, whose norm is 0 whatever it is: its gradient, a
+  // difference of two equal terms, would be their rounding, times 1 / sqrt(eps).
   __device__ __forceinline__ void params(const float* p, f8 (&v)[K], int fields) const {
+    const bool zero = scalar && m == 1.f;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int c = 0; c < 8; ++c) v[k][c] = p ? p[min(f0 + field(k, c), fields - 1)] : 1.f;
+      for (int c = 0; c < 8; ++c) v[k][c] = zero ? 0.f : p ? p[min(f0 + field(k, c), fields - 1)] : 1.f;
   }
 
   // The checkpoint of row r: int8 values at q, exponent bytes at b; of the chunks of the first `entries` entries.

@@ -114,3 +114,34 @@ def test_parameter_sums_that_cancel(name, n, dtype):
     alone = P.residual_backward(f, P.pack(full, y), P.pack(f, h), dh, dx, sc, gp, gn, EPS)
     for k in (2, 3, 4):
         assert torch.equal(got[k], want[k]) and torch.equal(packed[k], alone[k])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("eps", [1e-5, 1e-30])
+@pytest.mark.parametrize("f", [((0, 1),), ((1, 1),), ((0, 1), (1, 9)), ((0, 12), (0, 1), (2, 1)), ((1, 200), (0, 1))])
+def test_an_entry_of_one_scalar_has_no_gradient(f, eps, dtype):
+    """Its norm is 0 whatever it is, so nothing comes back through it, not even rounding (which 1 / sqrt(eps) would
+    make large); one gate is such an entry too."""
+    full = os_.gate_fields(f)
+    C, S, n, rng = channels(f), channels(full), 5, np.random.default_rng(4)
+    y, h, dh, dx = (dev(rng.standard_normal((n, c)), dtype) for c in (S, C, C, C))
+    sc, gp, gn = (dev(1 + 0.3 * rng.standard_normal(count(k))) for k in (f, full, f))
+    alone = [c for c, _, m, d in os_.entries(full) if m == d == 1]
+    own = [c for c in alone if c < C]
+    for x in (h, P.pack(f, h)):
+        assert not bool(P.site_norm_forward(f, x, gn, eps, dtype=dtype)[:, own].any())
+        got, dgain = P.site_norm_backward(f, x, dx, gn, eps, dres=dh)
+        assert torch.equal(got[:, own], dh[:, own])
+        assert not bool(P.site_norm_backward(f, x, dx, None, eps)[0][:, own].any())
+        assert bool(torch.isfinite(dgain).all())
+    for args in ((y, h), (P.pack(full, y), P.pack(f, h))):
+        for params in ((sc, gp, gn), (None, None, None)):
+            dy, dhi, ds, dp, dn = P.residual_backward(f, *args, dh, dx, *params, eps)
+            assert alone and not bool(dy[:, alone].any()) and torch.equal(dhi[:, own], dh[:, own])
+        ho = P.residual_forward(f, y, h, sc, gp, gn, eps)[0]
+        assert torch.equal(ho[:, own], h[:, own])
+    # a NaN or an infinity there is still one
+    bad = h.clone()
+    bad[0], bad[1] = float("nan"), float("inf")
+    assert bool(torch.isnan(P.site_norm_forward(f, bad, gn, eps)[:2, own]).all())
+    assert bool(torch.isnan(P.site_norm_backward(f, bad, dx, gn, eps)[0][:2, own]).all())
