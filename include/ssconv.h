@@ -360,7 +360,8 @@ int ssconv_site_norm_backward(const ssconv_fields* fields /*host*/, const ssconv
  * h_out and dx [n, C] = gradient of x_out (NULL where there was none; h_out may then
  * be NULL): dy [n, C + G], dh_in [n, C] = gradient of h, and dgain_post, dscale,
  * dgain_next (fp32, each NULL to skip; dgain_next NULL without dx), summed over the
- * rows as the norm's dgain.  relu'(0) = 0.  dh_in may be dh's or dx's buffer.
+ * rows as the norm's dgain.  relu'(0) = 0, and where relu' is 0 an infinity or a NaN of
+ * the gradient does not pass.  dh_in may be dh's or dx's buffer.
  * workspace: as for the norm, ssconv_residual_workspace_size bytes, needed where
  * one of the three is given.  n = 0, alignment, overlap and errors as for the norm. */
 int ssconv_residual_forward(const ssconv_fields* fields /*host*/, const void* y, const void* h, ssconv_dtype dtype,

@@ -99,7 +99,7 @@ def residual_backward(fields, y, h_out, dh, dx=None, scale=None, gain_post=None,
     C = f.shape[1]
     dg = dh * spread(fields, scale)
     du, g = np.zeros_like(u), C
-    du[:, :C] = dg * f
+    du[:, :C] = np.where(f == 0, 0, dg * f)   # a closed relu is a selection (sigmoids are above 0)
     for c, _, m, d in entries(fields):
         if d > 1:
             s = 1 / (1 + np.exp(-u[:, g:g + m]))

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kSiteNT, tail_bwd_per_cu(L, K, RAG)) void tail_bwd_
       for (int c = 0; c < 8; ++c) {
         const float u = y[k][c] * gp[k][c];
         prod[c] = e[k][c] * u;
-        e[k][c] *= u > 0.f || !w.scalar ? f[k][c] : 0.f;
+        e[k][c] = u > 0.f || !w.scalar ? e[k][c] * f[k][c] : 0.f;  // a closed relu stops infinities and NaN too
       }
       if (G && main[k] && !w.scalar) lds_put(w, k, buf, prod);
     }

@@ -145,3 +145,26 @@ def test_an_entry_of_one_scalar_has_no_gradient(f, eps, dtype):
     bad[0], bad[1] = float("nan"), float("inf")
     assert bool(torch.isnan(P.site_norm_forward(f, bad, gn, eps)[:2, own]).all())
     assert bool(torch.isnan(P.site_norm_backward(f, bad, dx, gn, eps)[0][:2, own]).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", list(FIELDS))
+def test_what_a_closed_relu_stops(name, dtype):
+    """relu' is 0 or 1 by selection, as in the gate's own backward: where a scalar is closed, an infinity or a NaN of its
+    gradient goes past the block and not into it."""
+    f = FIELDS[name]
+    full = os_.gate_fields(f)
+    n, rng = 13, np.random.default_rng(5)
+    y, h, dh = (dev(rng.standard_normal((n, c)), dtype) for c in (channels(full), channels(f), channels(f)))
+    u = os_.norm_forward(full, host(y), None, EPS)
+    scalar = np.concatenate([np.full(m * d, d == 1) for _, _, m, d in os_.entries(f)])
+    rows, cols = np.nonzero((u[:, :channels(f)] < -0.01) & scalar)
+    assert len(rows) > 5
+    at = torch.from_numpy(rows).to(DEV), torch.from_numpy(cols).to(DEV)
+    zero, bad = dh.clone(), dh.clone()
+    zero[at] = 0
+    bad[at] = torch.tensor([float("inf"), -float("inf"), float("nan")], dtype=dtype, device=DEV).repeat(len(rows))[:len(rows)]
+    want = P.residual_backward(f, y, h, zero, eps=EPS)
+    got = P.residual_backward(f, y, h, bad, eps=EPS)
+    assert torch.equal(got[0], want[0]) and bool(torch.isfinite(got[0]).all())
+    assert torch.equal(got[1].nan_to_num(7, 8, 9), bad.nan_to_num(7, 8, 9))
