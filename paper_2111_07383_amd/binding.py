@@ -379,9 +379,16 @@ class _Table:
         return self._full
 
 
+def _whole(v) -> int:
+    i = int(v)
+    if i != v or abs(i) >= 1 << 31:
+        raise ValueError(f"orders and multiplicities are whole numbers of 32 bits, got {v!r}")
+    return i
+
+
 @lru_cache(maxsize=256)
 def _table_of(fields) -> _Table:
-    fields = tuple((int(l), int(m)) for l, m in fields)
+    fields = tuple((_whole(l), _whole(m)) for l, m in fields)
     if not 1 <= len(fields) <= MAX_ENTRIES:
         raise ValueError(f"a field list has 1 to {MAX_ENTRIES} entries")
     return _Table(fields)
