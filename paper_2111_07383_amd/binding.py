@@ -498,7 +498,11 @@ def _workspace(ws: Optional[torch.Tensor], need: int, dev: int, device) -> Optio
 
 
 def _raw_stream(stream, dev: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, the current device is cuda:{dev}")
+    return stream.cuda_stream
 
 
 def pack(fields: FieldList, x: torch.Tensor, stream=None) -> Packed:

@@ -24,3 +24,13 @@ def test_whole_numbers_of_any_type():
     want = ((0, 3), (1, 2), (0, 2))
     for f in (((0, 3), (1, 2)), [[0, 3], [1, 2]], ((0.0, 3.0), (1, np.int64(2))), np.array([[0, 3], [1, 2]])):
         assert B.gate_fields(f) == want and all(type(v) is int for e in B.gate_fields(f) for v in e)
+
+
+def test_stream_of_another_device():
+    """The tensors are those of the current device, and a launch on another device's stream would reach them from there."""
+    class Stream:
+        device_index, cuda_stream = 1, 4096
+
+    assert B._raw_stream(Stream, 1) == 4096
+    with pytest.raises(ValueError):
+        B._raw_stream(Stream, 0)
