@@ -284,7 +284,10 @@ int launch(const KgradRows& G, const KgradRows& F, int cin, int cout, const ssco
 // in equal pieces the training step of that layer 1634 -> 1594).
 // `whole` on one 128 x 128 tile of split rows: one round where its lists are short, whose fill and partials then weigh
 // more than the rows (3x3x3, 104 -> 128: 13.7k sites, 265k pairs 118 us in four rounds, 94 in one;
-// 22.6k, 96 -> 120 channels 132 and 111; 104 -> 128 again: 70k, 1.4M 297 and 280; 310k, 6M 1288 and 1293).
+// 22.6k, 96 -> 120 channels 132 and 111; 104 -> 128 again: 70k, 1.4M 297 and 280; 310k, 6M 1288 and 1293).  Not where
+// one round is fewer than four slices of every list, as above: split_kgrad_wins takes it for half as slow again there and
+// leaves the call to the ring kernel (5x5x5, ring kernel and four rounds, with the rows' expansion: 71 -> 87 channels,
+// 1.03M pairs 262 and 216; 104 -> 128, 1.04M 309 and 252, 1.34M 382 and 318).
 // `whole` (bf16): tiles of 256 x 224 and 256 x 256 as well, which hold the kernel of a residual block of 208 channels and
 // its 48 gates at once; in 128 x 128 tiles every row is gathered twice (103.7k sites, 1.93M pairs, 208 -> 256: 414 us).
 KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout, bool whole) {
@@ -303,7 +306,8 @@ KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout, bo
   const int tiles = best.mtiles * best.ntiles;
   const int64_t by_pairs = rb->n_pairs / 256;
   int64_t most = parts == 3 ? 1024 : best.wm < 7 || rb->n_pairs >= 4000000 ? 512 : 256;
-  if (whole && parts == 3 && best.wm == 4 && best.wn == 4 && tiles == 1 && rb->n_pairs < 1500000) most = 256;
+  if (whole && parts == 3 && best.wm == 4 && best.wn == 4 && tiles == 1 && rb->n_pairs < 1500000 && 4 * rb->K <= 256)
+    most = 256;
   best.units = (int)std::max<int64_t>(1, std::min<int64_t>(most / tiles, by_pairs));
   return best;
 }
