@@ -2,6 +2,12 @@
 import numpy as np
 import pytest
 
+from cases import rel_err
+from oracle import conv as oc
+from oracle import rulebook as orb
+from oracle import site as os_
+from workloads.configs import LayerSpec
+
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
@@ -35,4 +41,72 @@ def test_many_offsets_keep_their_slices():
     p = P.pack(F104, x)
     got = P.backward_packed(p, g, rb, W, desc, basis, need_feats=False)[1]
     assert torch.equal(got, P.backward(P.unpack(p, torch.float32), g, rb, W, desc, basis, need_feats=False)[1])
+    rb.close()
+
+
+@pytest.fixture
+def variant():
+    """Sets the kernel override, and takes it back."""
+    yield lambda v: P.debug_set(3, v)
+    P.debug_set(3, 0)
+
+
+# fields, kernel size, sites drawn, grid, override: 0 where the rule itself is to take the three parts, 13 where a case is
+# smaller than it asks for
+CASES = {
+    "f104_k3_rule": (F104, 3, 60000, 24, 0),
+    "f104_k3": (F104, 3, 900, 10, 13),
+    "f104_k5": (F104, 5, 500, 9, 13),
+    "ragged_k3": (((0, 13), (1, 11), (2, 5)), 3, 700, 10, 13),
+    "f36_k3": (((0, 4), (1, 4), (2, 4)), 3, 300, 8, 13),
+    "f208_k3": (((0, 32), (1, 32), (2, 16)), 3, 400, 8, 13),
+    "one_site": (((0, 4), (1, 1)), 3, 1, 4, 13),
+}
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("name", list(CASES))
+def test_three_parts(name, norm, variant):
+    """Against the fp64 oracle and against ssconv_backward of the same rows, and in one workspace between calls whose
+    gradients (3e38, infinity) do not split: what those leave there the next one does not see."""
+    f, ks, n, grid, force = CASES[name]
+    rng = np.random.default_rng(n)
+    rb, desc, basis, W, x, g = layer(rng, f, ks, n, grid)
+    C, S = P.n_channels(f), P.n_channels(P.gate_fields(f))
+    gain = torch.from_numpy((1 + 0.2 * rng.standard_normal(sum(m for _, m in f))).astype(np.float32)).to(DEV)
+    kw = dict(norm=True, gain=gain) if norm else {}
+    variant(7)
+    other = P.backward_packed_workspace_size(rb, torch.float32, C, S)
+    variant(13)
+    size = P.backward_packed_workspace_size(rb, torch.float32, C, S)
+    variant(force)
+    assert P.backward_packed_workspace_size(rb, torch.float32, C, S) == size != other   # the route that is meant
+    p = P.pack(f, x)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+    call = lambda g: P.backward_packed(p, g, rb, W, desc, basis, need_feats=False, workspace=ws, **kw)[1]  # noqa: E731
+    got = call(g)
+    for bad in (3e38, float("inf")):
+        b = g.clone()
+        b[-1, 3] = bad
+        assert not torch.equal(call(b), got)
+        assert torch.equal(call(g), got)
+    rows = P.site_norm_forward(f, p, gain, dtype=torch.float32) if norm else P.unpack(p, torch.float32)
+    plain = P.backward(rows, g, rb, W, desc, basis, need_feats=False)[1]
+
+    coords = random_sites(np.random.default_rng(n), n, grid)
+    spec = LayerSpec(ks, 1, True, f, P.gate_fields(f), shells=tuple(float(i) for i in range(ks // 2 + 1)), gated=True)
+    lay, R = oc.Layer(spec), orb.rulebook(coords, coords, ks, 1)
+    v = os_.unpack(f, *os_.pack(f, x.double().cpu().numpy()))
+    if norm:
+        v = os_.norm_forward(f, v, gain.double().cpu().numpy())
+    gh, shape = g.double().cpu().numpy(), (ks ** 3, S, C)
+    want = oc.synth_adjoint(spec, lay.basis, oc.grad_kappa(v, gh, R, shape))
+    assert rel_err(got.cpu().numpy(), want) < 1e-4 and rel_err(plain.cpu().numpy(), want) < 1e-4
+    # both sums of at most `most` products in fp32, in whatever order, each off by at most that many 2^-24 of the sum of
+    # their magnitudes (1.01: second order, and the basis in fp32); 8 for the products of parts that are left out, under
+    # 2^-24 of the whole product, and for the rows' own roundings
+    most = 2 * max(len(r) for r in R) + max(b[0].size for b in lay.basis.values()) + 8
+    size = oc.grad_kappa(np.abs(v), np.abs(gh), R, shape)
+    bound = 2.02 * most * 2.0 ** -24 * oc.synth_adjoint(spec, {k: np.abs(b) for k, b in lay.basis.items()}, size)
+    assert (np.abs((got - plain).double().cpu().numpy()) <= bound).all()
     rb.close()
