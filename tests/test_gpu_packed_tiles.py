@@ -110,3 +110,44 @@ def test_three_parts(name, norm, variant):
     bound = 2.02 * most * 2.0 ** -24 * oc.synth_adjoint(spec, {k: np.abs(b) for k, b in lay.basis.items()}, size)
     assert (np.abs((got - plain).double().cpu().numpy()) <= bound).all()
     rb.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("norm", [False, True])
+def test_streams_and_graphs(norm, dtype, variant):
+    """Both gradients on a given stream and captured twice: every replay has the bits of the eager call, with other work and
+    another call whose gradient does not split between them, and follows new values in the captured buffers."""
+    variant(13)
+    rng = np.random.default_rng(5)
+    rb, desc, basis, W, x, g = layer(rng, F104, 3, 900, 10)
+    x, g = x.to(dtype), g.to(dtype)
+    W = (torch.from_numpy(rng.standard_normal(tuple(W.shape)).astype(np.float32)).to(DEV) / 60).to(dtype)
+    p = P.pack(F104, x)
+    call = lambda g, stream=None: P.backward_packed(p, g, rb, W, desc, basis, norm=norm, eps=1e-5, stream=stream)  # noqa: E731
+    ref = call(g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = call(g, side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(ref, got))
+    graphs, outs = [], []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(call(g))
+    bad = g.clone()
+    bad[3, 5] = 3e38
+    for step in range(4):
+        for o in outs:
+            for t in o:
+                t.fill_(7)
+        for graph in graphs:
+            graph.replay()
+        call(bad)
+        want = call(g)
+        torch.cuda.synchronize()
+        for o in outs:
+            assert all(torch.equal(a, b) for a, b in zip(o, want))
+        g.mul_(-0.5 if step else 1)
+        p.q.add_(1)
+    rb.close()
