@@ -211,7 +211,7 @@ extern "C" size_t ssconv_backward_packed_workspace_size(ssconv_rulebook_t rb, ss
 // The rows are expanded in front of the kernel gradient rather than in its loads: a row is read by n_pairs / n_in
 // pairs and would be normed, or at least scaled and rounded, that often, 20 VALU instructions for the 8 values of a
 // lane where a step of the kernel has 56 MFMAs for 7 such operands (expansion of 103.7k sites of 208 channels: 12 of
-// the call's us).
+// the call's 231 us).
 extern "C" int ssconv_backward_packed(const ssconv_fields* fields_in, const int8_t* q, const uint8_t* exps, int norm,
                                       double eps, const float* gain, const void* grad_out, ssconv_dtype dtype, int cout,
                                       ssconv_rulebook_t rb, const void* W, const ssconv_basis_desc* desc,

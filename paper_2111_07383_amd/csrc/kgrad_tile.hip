@@ -289,7 +289,8 @@ int launch(const KgradRows& G, const KgradRows& F, int cin, int cout, const ssco
 // leaves the call to the ring kernel (5x5x5, ring kernel and four rounds, with the rows' expansion: 71 -> 87 channels,
 // 1.03M pairs 262 and 216; 104 -> 128, 1.04M 309 and 252, 1.34M 382 and 318).
 // `whole` (bf16): tiles of 256 x 224 and 256 x 256 as well, which hold the kernel of a residual block of 208 channels and
-// its 48 gates at once; in 128 x 128 tiles every row is gathered twice (103.7k sites, 1.93M pairs, 208 -> 256: 414 us).
+// its 48 gates at once; in 128 x 128 tiles every row is gathered twice (103.7k sites, 1.93M pairs, 208 -> 256, coefficient
+// gradient: 466 us from rows on 128 x 128 tiles, 234 from a checkpoint on 256 x 224).
 KgradTile kgrad_tile(const ssconv_rulebook* rb, int parts, int cin, int cout, bool whole) {
   static const int shapes[][2] = {{2, 2}, {2, 4}, {4, 2}, {4, 4}, {7, 7}, {8, 7}, {8, 8}};
   KgradTile best{};

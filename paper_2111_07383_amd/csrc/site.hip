@@ -63,8 +63,8 @@ struct ReduceArgs {
 
 // Gradients of up to three parameters: out[f] = sum of the workgroups' partial sums over the components of field f, in
 // fp64 and a fixed order.  A workgroup takes as many fields of an entry as 16 channels hold: 64 slices of the rows of
-// partials (up to 2048, which lie in the L2s) are read side by side, 64 bytes a row (one workgroup a field and a
-// component at a time, a cache line for 4 bytes: 13.6 us for 2048 rows of 208 channels).
+// partials (up to 1536, which lie in the L2s) are read side by side, 64 bytes a row: 6.2 us for 1536 rows of 208
+// channels (one workgroup a field and a component at a time, a cache line for 4 bytes: 13.6 us for 2048 rows).
 constexpr int kReduceNT = 1024, kReduceC = 16;
 inline int fields_per_group(int l) { return kReduceC / (2 * l + 1); }
 

@@ -37,10 +37,9 @@ struct SiteTab {
 // gated: the gates of the fields of order > 0 as one more entry.
 int make_sitetab(const ssconv_fields* f, bool gated, SiteTab* t);
 
-// Lanes per row: the fewest that hold a row with one chunk each, or 64 with two or three.  Twice as many leave half of a
+// Lanes per row: the fewest that hold a row with one chunk each, or 64 with two or four.  Twice as many leave half of a
 // wavefront idle (backward of a residual tail, bf16: 150k rows of 36 channels on 8 lanes 53 us, on 16 86; 100k of 104 on
-// 16 38, on 32 55).  More chunks a lane than a row needs cost more than idle lanes, and their sums go entry by entry (60k
-// rows of 480 channels and 96 gates with two chunks 198 us, with three 402).
+// 16 38, on 32 55).  K is doubled only where 64 lanes are too few (SiteTab has both sides).
 inline int site_lanes(const SiteTab& t) {
   const int c = t.t0[t.n];
   return c <= 8 ? 8 : c <= 16 ? 16 : c <= 32 ? 32 : 64;
