@@ -579,10 +579,10 @@ int kgrad_f32_units_want(const ssconv_rulebook* rb, int cin, int cout, bool whol
   double len = 256;
   // `whole`: where up to four tiles hold the kernel, the length at which four pairs of a task take as long as the
   // partials they need (times of split_kgrad_wins), if that is shorter (fp32 gradients from checkpoints with 256 pairs
-  // and so, us: 36 -> 44 channels, 4.9k pairs 54 and 31; 32 -> 40, 19k 43 and 27; 71 -> 87, 12k 47 and 35; 52 -> 64, 99k 58 and 49; 104 ->
-  // 128, 19k 50 and 45; in eight and more tiles 208 -> 256, 37k 97 and 86, 12k 66 and 67, 312 -> 384, 37k 154 and 163;
-  // 5x5x5, 256 pairs from rows and so from checkpoints: 36 -> 44, 20k 52 and 41, 88k 65 and 49; 104 -> 128, 22k 84 and 66,
-  // 84k 99 and 87)
+  // and so, us: 36 -> 44 channels, 4.9k pairs 54 and 31; 32 -> 40, 19k 43 and 27; 71 -> 87, 12k 47 and 35; 52 -> 64, 99k
+  // 58 and 49; 104 -> 128, 19k 50 and 45; in eight and more tiles 208 -> 256, 37k 97 and 86, 12k 66 and 67, 312 -> 384,
+  // 37k 154 and 163; 5x5x5, 256 pairs from rows and so from checkpoints: 36 -> 44, 20k 52 and 41, 88k 65 and 49;
+  // 104 -> 128, 22k 84 and 66, 84k 99 and 87)
   if (whole && p.mtiles * p.ntiles <= 4) {
     const double step = 0.15 + 0.018 * p.wmb * p.wnb, partial = 8.0 * cin * cout / 4.5e6;
     len = std::min(len, std::max(16.0, std::sqrt(4.0 * rb->n_pairs * partial / step)));

@@ -469,7 +469,8 @@ _Pragma("unroll") for (int a = 0; a < N; ++a) {      \
       } else {
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-          if (counts(k, c)) q[c] = (int8_t)(byte == 255 ? 0u : __float_as_uint(fmaf(pack_hold(x[k][c]), scale, 12582912.f)));
+          if (counts(k, c))
+            q[c] = (int8_t)(byte == 255 ? 0u : __float_as_uint(fmaf(pack_hold(x[k][c]), scale, 12582912.f)));
       }
     }
     if (first) b0[(uint32_t)(__umul24(r, B) + blk[0])] = (uint8_t)byte;

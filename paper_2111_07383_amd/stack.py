@@ -37,7 +37,8 @@ def regular_fields(layer):
 @dataclass
 class Stack:
     """``checkpoint``: the forward keeps every layer's input and convolution output as 8-bit checkpoints
-    (their values are within 1/127 of the largest of 32 channels), and the gradients are taken at those."""
+    (their values are within 1/127 of the largest of 32 channels), and the gradients are taken at those; layers then
+    have at most 1024 channels."""
     layers: List[LayerState] = field(default_factory=list)
     dtype: torch.dtype = torch.float32
     checkpoint: bool = False
